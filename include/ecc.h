@@ -350,6 +350,68 @@ int ecc_count_nonfinite(const void* grid, int64_t n, ecc_dtype dtype, unsigned l
                         void* hip_stream);
 
 /*
+ * Group normalisation with an activation, channels last: the layer that stands before a field is made for the soft curves
+ * (features [batch][D][H][W][channels] or [batch][H][W][channels], `points` = D H W), or behind them (curves as channels,
+ * points = 1).  Over the points and the channels of each of `groups` equal runs of channels:
+ *     xhat = (x - mean) / sqrt(var + eps)       (var: the mean of the squares about the mean)
+ *     y    = act(xhat weight[c] + bias[c]),     act: ECC_ACT_NONE, ECC_ACT_RELU, ECC_ACT_SILU (v / (1 + exp(-v)))
+ *   x, y         device [batch][points][channels] of type `dtype`: ECC_F32, ECC_F16 or ECC_BF16, aligned to their element
+ *   weight, bias device float32 [channels], either NULL (ones, zeros)
+ *   stats        device double [batch][groups][2], out: mean and 1 / sqrt(var + eps) for ecc_norm_bwd, or NULL
+ * ecc_norm_bwd: from x, stats and the upstream gradient grad_y (as y) the gradients grad_x (as x), grad_weight and
+ * grad_bias (device float32 [channels]); any of the three may be NULL, not all.  The derivative of relu at 0 is 0.
+ * Sums are float32 within a block's share and float64 beyond, in a fixed order: repeated calls give the same bits.  Outputs
+ * must not overlap inputs.  A NaN or Inf spoils its own group of its own item, and the gradients of its channels.
+ *   1 <= channels <= ECC_MAX_CHANNELS, groups a divisor of channels, eps finite and >= 0
+ *   workspace    ecc_norm_workspace_bytes() bytes, 256-byte aligned, enough for either call
+ */
+#define ECC_ACT_NONE 0
+#define ECC_ACT_RELU 1
+#define ECC_ACT_SILU 2
+#define ECC_MAX_CHANNELS 65536
+size_t ecc_norm_workspace_bytes(int64_t batch, int64_t points, int channels, int groups);
+int ecc_norm_fwd(const void* x, int64_t batch, int64_t points, int channels, int groups, ecc_dtype dtype,
+                 const float* weight, const float* bias, float eps, int act, void* y, double* stats, void* workspace,
+                 size_t workspace_bytes, void* hip_stream);
+int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t points, int channels, int groups,
+                 ecc_dtype dtype, const float* weight, const float* bias, int act, const double* stats, void* grad_x,
+                 float* grad_weight, float* grad_bias, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Softmax cross entropy of a linear head without a bias: what curves (rows = items) or the features of every voxel
+ * (rows = voxels) cost against their labels.  With z_iv = <hidden_i, weight_v>:
+ *     loss_i = log sum_v exp z_iv - z_{i, labels[i]},     0 for a row whose label is `ignore_index`
+ * The logits are never held whole: the forward pass keeps a maximum and a sum for each row and run of classes, the backward
+ * pass forms the logits' gradient of one run of classes at a time.
+ *   hidden       device [rows][dim], weight device [classes][dim], both of type `dtype`: ECC_F32, ECC_F16 or ECC_BF16,
+ *                aligned to their element
+ *   labels       device int64 [rows].  A label that is neither `ignore_index` nor in 0 .. classes - 1 makes its row's loss
+ *                and gradients NaN
+ *   reduction    ECC_MEAN (over the rows that are not left out; 0 where there are none), ECC_SUM, or ECC_EACH
+ *   loss         device float32 out: [1], or [rows] for ECC_EACH
+ *   lse          device float32 [rows] out, log sum_v exp z_iv for ecc_xent_bwd, or NULL
+ *   counted      device int64 [1] out, the number of rows that are not left out, for ecc_xent_bwd; NULL with lse
+ * ecc_xent_bwd: grad_loss (device float32, [1] or [rows] as the loss) carried on to grad_hidden and grad_weight (as hidden
+ * and weight), either of which may be NULL.  Rows that are left out get zeros and, whatever their features hold, add
+ * nothing to grad_weight.
+ * Products are summed in float32; the logits' gradient is rounded to `dtype` before its products (float32: held whole).
+ * Orders are fixed: repeated calls give the same bits.
+ *   1 <= rows, classes < 2^31, 1 <= dim <= ECC_MAX_CHANNELS;  workspace: 256-byte aligned, of ecc_xent_workspace_bytes()
+ *   bytes (backward: 0 or 1)
+ */
+#define ECC_MEAN 0
+#define ECC_SUM 1
+#define ECC_EACH 2
+size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtype dtype, int backward);
+int ecc_xent_fwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, float* loss, float* lse, int64_t* counted,
+                 void* workspace, size_t workspace_bytes, void* hip_stream);
+int ecc_xent_bwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, const float* lse, const int64_t* counted,
+                 const float* grad_loss, void* grad_hidden, void* grad_weight, void* workspace, size_t workspace_bytes,
+                 void* hip_stream);
+
+/*
  * Test aid (not part of the method): forces the fall-back kernels on shapes
  * that would otherwise take the fast ones, so that tests can compare every
  * path with the oracle on the same inputs.  `mask` is an OR of

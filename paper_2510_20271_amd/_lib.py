@@ -61,6 +61,16 @@ SIGNATURES = {
                                     ctypes.c_float, ctypes.c_int, ctypes.POINTER(ctypes.c_double), c_vp, c_vp,
                                     ctypes.c_size_t, c_vp]),
     "ecc_count_nonfinite": (ctypes.c_int, [c_vp, c_i64, ctypes.c_int, c_vp, c_vp]),
+    "ecc_norm_workspace_bytes": (ctypes.c_size_t, [c_i64, c_i64, ctypes.c_int, ctypes.c_int]),
+    "ecc_norm_fwd": (ctypes.c_int, [c_vp, c_i64, c_i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, c_vp, c_vp,
+                                    ctypes.c_float, ctypes.c_int, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "ecc_norm_bwd": (ctypes.c_int, [c_vp, c_vp, c_i64, c_i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, c_vp, c_vp,
+                                    ctypes.c_int, c_vp, c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "ecc_xent_workspace_bytes": (ctypes.c_size_t, [c_i64, ctypes.c_int, c_i64, ctypes.c_int, ctypes.c_int]),
+    "ecc_xent_fwd": (ctypes.c_int, [c_vp, c_vp, c_vp, c_i64, ctypes.c_int, c_i64, ctypes.c_int, c_i64, ctypes.c_int,
+                                    c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "ecc_xent_bwd": (ctypes.c_int, [c_vp, c_vp, c_vp, c_i64, ctypes.c_int, c_i64, ctypes.c_int, c_i64, ctypes.c_int,
+                                    c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
     "ecc_debug_force": (ctypes.c_uint, [ctypes.c_uint]),
     "ecc_profile_begin": (ctypes.c_int, [ctypes.c_int]),
     "ecc_profile_end": (ctypes.c_int, [ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int)]),

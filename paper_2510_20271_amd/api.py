@@ -346,6 +346,170 @@ def ecc_count_nonfinite(grid: torch.Tensor, count=None):
     return count
 
 
+ECC_ACT_NONE, ECC_ACT_RELU, ECC_ACT_SILU = 0, 1, 2
+_ACTS = {"none": ECC_ACT_NONE, "relu": ECC_ACT_RELU, "silu": ECC_ACT_SILU}
+ECC_MEAN, ECC_SUM, ECC_EACH = 0, 1, 2
+_REDUCTIONS = {"mean": ECC_MEAN, "sum": ECC_SUM, "none": ECC_EACH}
+_OPERATOR_DTYPES = {torch.float32: ECC_F32, torch.float16: ECC_F16, torch.bfloat16: ECC_BF16}
+
+
+def _one_of(table, value, name):
+    if value not in table:
+        raise ValueError(f"{name} must be one of {', '.join(map(str, table))}, got {value!r}")
+    return table[value]
+
+
+def _like(name, t, shape, dtype, device):
+    """Refuses a tensor of another type, shape or device (None passes)."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)} on {device}, got {t.dtype} of shape "
+                         f"{tuple(t.shape)} on {t.device}")
+
+
+def _on_current_device(t):
+    """The stream is the current device's, so that is where the tensors have to be."""
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors must be on the current device, got {t.device}")
+
+
+def _room(need: int, device) -> torch.Tensor:
+    """Workspace of one call, from torch's allocator: it belongs to the current stream, or to the graph being captured."""
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def ecc_norm_workspace_bytes(batch: int, points: int, channels: int, groups: int) -> int:
+    return int(_lib.load().ecc_norm_workspace_bytes(batch, points, channels, groups))
+
+
+def _norm_args(x, groups, weight, bias, act):
+    """Sizes, type and activation of a normalisation; x [batch, ..., channels]."""
+    if x.dim() < 2:
+        raise ValueError("x must be [batch, (points,) channels]")
+    dtype = _one_of(_OPERATOR_DTYPES, x.dtype, "the type of x")
+    batch, channels = x.shape[0], x.shape[-1]
+    points = 1
+    for k in x.shape[1:-1]:
+        points *= k
+    _like("weight", weight, (channels,), torch.float32, x.device)
+    _like("bias", bias, (channels,), torch.float32, x.device)
+    return batch, points, channels, int(groups), dtype, _one_of(_ACTS, act, "act")
+
+
+def ecc_norm_fwd(x, groups, weight=None, bias=None, eps=1e-5, act="silu", y=None, stats=None, workspace=None,
+                 keep=True):
+    """Group norm and activation of x [batch, (D,) H, W, channels] or [batch, channels] (float32 / float16 / bfloat16,
+    contiguous), weight and bias float32 [channels].  Returns (y, stats); stats [batch, groups, 2] float64 is what
+    ecc_norm_bwd needs, None with keep=False."""
+    _need_device(x, weight, bias, y, stats, workspace)
+    _on_current_device(x)
+    batch, points, channels, groups, dtype, code = _norm_args(x, groups, weight, bias, act)
+    _like("y", y, x.shape, x.dtype, x.device)
+    _like("stats", stats, (batch, groups, 2), torch.float64, x.device)
+    if y is None:
+        y = torch.empty_like(x)
+    if stats is None and keep:
+        stats = torch.empty((batch, max(groups, 0), 2), dtype=torch.float64, device=x.device)
+    if workspace is None:
+        workspace = _room(_kept_bytes(ecc_norm_workspace_bytes, batch, points, channels, groups), x.device)
+    _check(_lib.load().ecc_norm_fwd(_ptr(x), batch, points, channels, groups, dtype, _ptr(weight), _ptr(bias),
+                                    float(eps), code, _ptr(y), _ptr(stats), _ptr(workspace), workspace.numel(),
+                                    _stream()))
+    return y, stats
+
+
+def ecc_norm_bwd(x, grad_y, groups, stats, weight=None, bias=None, act="silu", grad_x=None, grad_weight=None,
+                 grad_bias=None, workspace=None, skip=()):
+    """(grad_x, grad_weight, grad_bias) of ecc_norm_fwd from the upstream gradient and the stats it returned.
+    skip: names among "grad_x", "grad_weight", "grad_bias" of outputs that are not wanted; not all three."""
+    _need_device(x, grad_y, stats, weight, bias, grad_x, grad_weight, grad_bias, workspace)
+    _on_current_device(x)
+    batch, points, channels, groups, dtype, code = _norm_args(x, groups, weight, bias, act)
+    _like("grad_y", grad_y, x.shape, x.dtype, x.device)
+    _like("stats", stats, (batch, groups, 2), torch.float64, x.device)
+    _like("grad_x", grad_x, x.shape, x.dtype, x.device)
+    _like("grad_weight", grad_weight, (channels,), torch.float32, x.device)
+    _like("grad_bias", grad_bias, (channels,), torch.float32, x.device)
+    if grad_x is None and "grad_x" not in skip:
+        grad_x = torch.empty_like(x)
+    if grad_weight is None and "grad_weight" not in skip:
+        grad_weight = torch.empty(channels, dtype=torch.float32, device=x.device)
+    if grad_bias is None and "grad_bias" not in skip:
+        grad_bias = torch.empty(channels, dtype=torch.float32, device=x.device)
+    if workspace is None:
+        workspace = _room(_kept_bytes(ecc_norm_workspace_bytes, batch, points, channels, groups), x.device)
+    _check(_lib.load().ecc_norm_bwd(_ptr(x), _ptr(grad_y), batch, points, channels, groups, dtype, _ptr(weight),
+                                    _ptr(bias), code, _ptr(stats), _ptr(grad_x), _ptr(grad_weight), _ptr(grad_bias),
+                                    _ptr(workspace), workspace.numel(), _stream()))
+    return grad_x, grad_weight, grad_bias
+
+
+def ecc_xent_workspace_bytes(rows: int, dim: int, classes: int, dtype: int, backward: bool) -> int:
+    return int(_lib.load().ecc_xent_workspace_bytes(rows, dim, classes, dtype, int(bool(backward))))
+
+
+def _xent_args(hidden, weight, labels, reduction):
+    if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
+        raise ValueError("hidden must be [rows, dim] and weight [classes, dim]")
+    dtype = _one_of(_OPERATOR_DTYPES, hidden.dtype, "the type of hidden")
+    rows, dim = hidden.shape
+    _like("weight", weight, weight.shape, hidden.dtype, hidden.device)
+    _like("labels", labels, (rows,), torch.int64, hidden.device)
+    return rows, dim, weight.shape[0], dtype, _one_of(_REDUCTIONS, reduction, "reduction")
+
+
+def ecc_xent_fwd(hidden, weight, labels, ignore_index=-100, reduction="mean", loss=None, lse=None, counted=None,
+                 workspace=None, keep=True):
+    """Cross entropy of the linear head z = hidden weight^T: hidden [rows, dim], weight [classes, dim] (float32 / float16
+    / bfloat16, contiguous), labels int64 [rows].  Returns (loss, lse, counted): loss float32, a scalar or [rows] with
+    reduction="none"; lse [rows] and counted (an int64 scalar) are what ecc_xent_bwd needs, None with keep=False."""
+    _need_device(hidden, weight, labels, loss, lse, counted, workspace)
+    _on_current_device(hidden)
+    rows, dim, classes, dtype, code = _xent_args(hidden, weight, labels, reduction)
+    dev = hidden.device
+    shape = (rows,) if code == ECC_EACH else ()
+    _like("loss", loss, shape, torch.float32, dev)
+    _like("lse", lse, (rows,), torch.float32, dev)
+    _like("counted", counted, (), torch.int64, dev)
+    if loss is None:
+        loss = torch.empty(shape, dtype=torch.float32, device=dev)
+    if keep and lse is None:
+        lse = torch.empty(rows, dtype=torch.float32, device=dev)
+    if keep and counted is None:
+        counted = torch.empty((), dtype=torch.int64, device=dev)
+    if workspace is None:
+        workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, False), dev)
+    _check(_lib.load().ecc_xent_fwd(_ptr(hidden), _ptr(weight), _ptr(labels), rows, dim, classes, dtype,
+                                    int(ignore_index), code, _ptr(loss), _ptr(lse), _ptr(counted), _ptr(workspace),
+                                    workspace.numel(), _stream()))
+    return loss, lse, counted
+
+
+def ecc_xent_bwd(hidden, weight, labels, grad_loss, lse, counted, ignore_index=-100, reduction="mean",
+                 grad_hidden=None, grad_weight=None, workspace=None, skip=()):
+    """(grad_hidden, grad_weight) of ecc_xent_fwd from the upstream gradient grad_loss (float32, as the loss) and what
+    it returned.  skip: the name of the output that is not wanted, if one is not."""
+    _need_device(hidden, weight, labels, grad_loss, lse, counted, grad_hidden, grad_weight, workspace)
+    _on_current_device(hidden)
+    rows, dim, classes, dtype, code = _xent_args(hidden, weight, labels, reduction)
+    dev = hidden.device
+    _like("grad_loss", grad_loss, (rows,) if code == ECC_EACH else (), torch.float32, dev)
+    _like("lse", lse, (rows,), torch.float32, dev)
+    _like("counted", counted, (), torch.int64, dev)
+    _like("grad_hidden", grad_hidden, hidden.shape, hidden.dtype, dev)
+    _like("grad_weight", grad_weight, weight.shape, weight.dtype, dev)
+    if grad_hidden is None and "grad_hidden" not in skip:
+        grad_hidden = torch.empty_like(hidden)
+    if grad_weight is None and "grad_weight" not in skip:
+        grad_weight = torch.empty_like(weight)
+    if workspace is None:
+        workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, True), dev)
+    _check(_lib.load().ecc_xent_bwd(_ptr(hidden), _ptr(weight), _ptr(labels), rows, dim, classes, dtype,
+                                    int(ignore_index), code, _ptr(lse), _ptr(counted), _ptr(grad_loss),
+                                    _ptr(grad_hidden), _ptr(grad_weight), _ptr(workspace), workspace.numel(),
+                                    _stream()))
+    return grad_hidden, grad_weight
+
+
 ECC_FORCE_GENERIC, ECC_FORCE_TWO_PASS, ECC_FORCE_SOFT_TILES, ECC_FORCE_NO_SMALL = 1, 2, 4, 8
 
 

@@ -10,6 +10,8 @@
 #include <mutex>
 
 #include "ecc_internal.h"
+#include "ecc_norm.h"
+#include "ecc_xent.h"
 
 // Scratch of ecc_hard_static: device memory that belongs to the library, one copy per GPU,
 // held until the process ends.  In host code the name is only a handle for
@@ -493,6 +495,141 @@ int ecc_count_nonfinite(const void* grid, int64_t n, ecc_dtype dtype, unsigned l
   if (reinterpret_cast<uintptr_t>(count) % 8) return fail(ECC_ERR_INVALID_ARG, "count is not 8-byte aligned");
   return device_status(ecc::launch_count_nonfinite(grid, n, dtype, count, static_cast<hipStream_t>(hip_stream)),
                        "ecc_count_nonfinite");
+}
+
+static int check_operator_dtype(int dtype) {
+  if (dtype != ECC_F32 && dtype != ECC_F16 && dtype != ECC_BF16)
+    return fail(ECC_ERR_INVALID_ARG, "unknown dtype %d (this entry point takes ECC_F32, ECC_F16, ECC_BF16)", dtype);
+  return ECC_OK;
+}
+// a required (or optional) array of elements of `size` bytes
+static int check_array(const void* p, const char* name, size_t size, bool optional = false) {
+  if (!p) return optional ? ECC_OK : fail(ECC_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % size) return fail(ECC_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, size);
+  return ECC_OK;
+}
+
+static int check_norm_sizes(int64_t batch, int64_t points, int channels, int groups) {
+  if (batch < 1) return fail(ECC_ERR_INVALID_ARG, "batch must be >= 1, got %lld", (long long)batch);
+  if (points < 1) return fail(ECC_ERR_INVALID_ARG, "points must be >= 1, got %lld", (long long)points);
+  if (channels < 1) return fail(ECC_ERR_INVALID_ARG, "channels must be >= 1, got %d", channels);
+  if (channels > ECC_MAX_CHANNELS)
+    return fail(ECC_ERR_UNSUPPORTED, "channels %d exceeds ECC_MAX_CHANNELS %d", channels, ECC_MAX_CHANNELS);
+  if (groups < 1 || channels % groups)
+    return fail(ECC_ERR_INVALID_ARG, "groups must divide the %d channels, got %d", channels, groups);
+  if (points > kMaxVertices / channels || batch > kMaxVertices / (points * channels))
+    return fail(ECC_ERR_UNSUPPORTED, "batch * points * channels exceeds 2^40");
+  if (batch > INT32_MAX / groups) return fail(ECC_ERR_UNSUPPORTED, "batch * groups exceeds 2^31 - 1");
+  return ECC_OK;
+}
+static int check_norm(const ecc::NormArgs& a, int dtype) {
+  int rc = check_norm_sizes(a.batch, a.points, a.C, a.G);
+  if (rc != ECC_OK || (rc = check_operator_dtype(dtype)) != ECC_OK) return rc;
+  if (a.act != ECC_ACT_NONE && a.act != ECC_ACT_RELU && a.act != ECC_ACT_SILU)
+    return fail(ECC_ERR_INVALID_ARG, "unknown activation %d", a.act);
+  if ((rc = check_array(a.x, "x", dtype_size(dtype))) != ECC_OK || (rc = check_array(a.w, "weight", 4, true)) != ECC_OK)
+    return rc;
+  return check_array(a.b, "bias", 4, true);
+}
+
+size_t ecc_norm_workspace_bytes(int64_t batch, int64_t points, int channels, int groups) {
+  if (check_norm_sizes(batch, points, channels, groups) != ECC_OK) return 0;
+  return ecc::norm_workspace_bytes(batch, points, channels, groups);
+}
+
+int ecc_norm_fwd(const void* x, int64_t batch, int64_t points, int channels, int groups, ecc_dtype dtype,
+                 const float* weight, const float* bias, float eps, int act, void* y, double* stats, void* workspace,
+                 size_t workspace_bytes, void* hip_stream) {
+  ecc::NormArgs a{};
+  a.x = x; a.w = weight; a.b = bias; a.y = y; a.stats = stats; a.ws = workspace;
+  a.batch = batch; a.points = points; a.C = channels; a.G = groups; a.act = act; a.eps = eps;
+  int rc = check_norm(a, dtype);
+  if (rc != ECC_OK) return rc;
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(ECC_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if ((rc = check_array(y, "y", dtype_size(dtype))) != ECC_OK || (rc = check_array(stats, "stats", 8, true)) != ECC_OK)
+    return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes, ecc::norm_workspace_bytes(batch, points, channels, groups))) != ECC_OK)
+    return rc;
+  return device_status(ecc::launch_norm_fwd(a, dtype, static_cast<hipStream_t>(hip_stream)), "ecc_norm_fwd");
+}
+
+int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t points, int channels, int groups,
+                 ecc_dtype dtype, const float* weight, const float* bias, int act, const double* stats, void* grad_x,
+                 float* grad_weight, float* grad_bias, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  ecc::NormArgs a{};
+  a.x = x; a.dy = grad_y; a.w = weight; a.b = bias; a.dx = grad_x; a.dw = grad_weight; a.db = grad_bias;
+  a.stats = const_cast<double*>(stats); a.ws = workspace;
+  a.batch = batch; a.points = points; a.C = channels; a.G = groups; a.act = act;
+  int rc = check_norm(a, dtype);
+  if (rc != ECC_OK) return rc;
+  const size_t size = dtype_size(dtype);
+  if ((rc = check_array(grad_y, "grad_y", size)) != ECC_OK || (rc = check_array(stats, "stats", 8)) != ECC_OK ||
+      (rc = check_array(grad_x, "grad_x", size, true)) != ECC_OK ||
+      (rc = check_array(grad_weight, "grad_weight", 4, true)) != ECC_OK ||
+      (rc = check_array(grad_bias, "grad_bias", 4, true)) != ECC_OK)
+    return rc;
+  if (!grad_x && !grad_weight && !grad_bias) return fail(ECC_ERR_INVALID_ARG, "every output is NULL");
+  if ((rc = check_workspace(workspace, workspace_bytes, ecc::norm_workspace_bytes(batch, points, channels, groups))) != ECC_OK)
+    return rc;
+  return device_status(ecc::launch_norm_bwd(a, dtype, static_cast<hipStream_t>(hip_stream)), "ecc_norm_bwd");
+}
+
+static int check_xent_sizes(int64_t rows, int dim, int64_t classes, int dtype) {
+  if (rows < 1 || classes < 1 || dim < 1)
+    return fail(ECC_ERR_INVALID_ARG, "rows, dim and classes must be >= 1, got %lld, %d, %lld", (long long)rows, dim,
+                (long long)classes);
+  if (rows > INT32_MAX || classes > INT32_MAX || dim > ECC_MAX_CHANNELS)
+    return fail(ECC_ERR_UNSUPPORTED, "rows and classes must be below 2^31 and dim at most %d", ECC_MAX_CHANNELS);
+  return check_operator_dtype(dtype);
+}
+static int check_xent(const ecc::XentArgs& a, int dtype, bool backward, size_t workspace_bytes) {
+  int rc = check_xent_sizes(a.rows, a.dim, a.classes, dtype);
+  if (rc != ECC_OK) return rc;
+  const size_t size = dtype_size(dtype);
+  if ((rc = check_array(a.h, "hidden", size)) != ECC_OK || (rc = check_array(a.w, "weight", size)) != ECC_OK ||
+      (rc = check_array(a.labels, "labels", 8)) != ECC_OK)
+    return rc;
+  if (a.reduction != ECC_MEAN && a.reduction != ECC_SUM && a.reduction != ECC_EACH)
+    return fail(ECC_ERR_INVALID_ARG, "unknown reduction %d", a.reduction);
+  if ((rc = check_array(a.lse, "lse", 4, !backward)) != ECC_OK) return rc;
+  if ((rc = check_array(a.counted, "counted", 8, !backward)) != ECC_OK) return rc;
+  if (!a.lse != !a.counted) return fail(ECC_ERR_INVALID_ARG, "lse and counted come together");
+  return check_workspace(a.ws, workspace_bytes, ecc::xent_workspace_bytes(a.rows, a.dim, a.classes, dtype, backward));
+}
+
+size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtype dtype, int backward) {
+  if (check_xent_sizes(rows, dim, classes, dtype) != ECC_OK) return 0;
+  return ecc::xent_workspace_bytes(rows, dim, classes, dtype, backward != 0);
+}
+
+int ecc_xent_fwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, float* loss, float* lse, int64_t* counted,
+                 void* workspace, size_t workspace_bytes, void* hip_stream) {
+  ecc::XentArgs a{};
+  a.h = hidden; a.w = weight; a.labels = labels; a.rows = rows; a.classes = classes; a.dim = dim;
+  a.reduction = reduction; a.ignore = ignore_index; a.loss = loss; a.lse = lse; a.counted = counted; a.ws = workspace;
+  int rc = check_array(loss, "loss", 4);
+  if (rc != ECC_OK || (rc = check_xent(a, dtype, false, workspace_bytes)) != ECC_OK) return rc;
+  return device_status(ecc::launch_xent_fwd(a, dtype, static_cast<hipStream_t>(hip_stream)), "ecc_xent_fwd");
+}
+
+int ecc_xent_bwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, const float* lse, const int64_t* counted,
+                 const float* grad_loss, void* grad_hidden, void* grad_weight, void* workspace, size_t workspace_bytes,
+                 void* hip_stream) {
+  ecc::XentArgs a{};
+  a.h = hidden; a.w = weight; a.labels = labels; a.rows = rows; a.classes = classes; a.dim = dim;
+  a.reduction = reduction; a.ignore = ignore_index; a.lse = const_cast<float*>(lse);
+  a.counted = const_cast<int64_t*>(counted); a.up = grad_loss; a.dh = grad_hidden; a.dw = grad_weight; a.ws = workspace;
+  int rc = check_xent(a, dtype, true, workspace_bytes);
+  if (rc != ECC_OK) return rc;
+  const size_t size = dtype_size(dtype);
+  if ((rc = check_array(grad_loss, "grad_loss", 4)) != ECC_OK ||
+      (rc = check_array(grad_hidden, "grad_hidden", size, true)) != ECC_OK ||
+      (rc = check_array(grad_weight, "grad_weight", size, true)) != ECC_OK)
+    return rc;
+  if (!grad_hidden && !grad_weight) return fail(ECC_ERR_INVALID_ARG, "every output is NULL");
+  return device_status(ecc::launch_xent_bwd(a, dtype, static_cast<hipStream_t>(hip_stream)), "ecc_xent_bwd");
 }
 
 int ecc_profile_begin(int max_launches) {

@@ -1,0 +1,248 @@
+"""The linear head's cross entropy against its plain form in 64 bits: shapes, types, reductions, gradients, edges."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2510_20271_amd import api
+from paper_2510_20271_amd.loss import LinearCrossEntropy, linear_cross_entropy
+from tests.operator_bounds import within, xent_reference
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+SHAPES = [  # rows, dim, classes
+    (1, 1, 1), (1, 1, 2), (2, 3, 5), (1, 64, 1000), (7, 16, 21), (64, 64, 64), (33, 30, 257), (129, 65, 131), (300, 128, 1000),
+    (1000, 8, 3), (17, 2050, 33), (5, 40, 20011), (520, 264, 300), (2100, 72, 21), (256, 512, 512), (1, 4096, 3001),
+    (70, 100, 8200), (4099, 33, 70),
+]
+
+
+def _data(n, d, V, dtype, seed=0, ignored=0.2):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    W = torch.randn(V, d, generator=gen, device="cuda") * d ** -0.5
+    labels = torch.randint(0, V, (n,), generator=gen, device="cuda")
+    h = 2 * torch.randn(n, d, generator=gen, device="cuda") + 8 * torch.rand(n, 1, generator=gen, device="cuda") * W[labels]
+    if n > 1:
+        labels[torch.rand(n, generator=gen, device="cuda") < ignored] = -100
+    up = 0.5 + torch.rand(n, generator=gen, device="cuda")
+    return h.to(dtype), W.to(dtype), labels, up
+
+
+def _check(h, W, labels, reduction, up, ignore=-100):
+    hr, Wr = h.clone().requires_grad_(True), W.clone().requires_grad_(True)
+    loss = linear_cross_entropy(hr, Wr, labels, ignore_index=ignore, reduction=reduction)
+    upstream = up if reduction == "none" else torch.tensor(0.75, device="cuda")
+    dh, dW = torch.autograd.grad(loss, (hr, Wr), upstream)
+    ref = xent_reference(h, W, labels, ignore, reduction, upstream)
+    assert loss.dtype == F32 and dh.dtype == h.dtype and dW.dtype == W.dtype
+    within(loss.detach(), ref[0], ref[1], "loss")
+    within(dh, ref[2], ref[3], "dhidden")
+    within(dW, ref[4], ref[5], "dweight")
+    with torch.no_grad():
+        assert torch.equal(linear_cross_entropy(h, W, labels, ignore_index=ignore, reduction=reduction), loss.detach())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,d,V", SHAPES)
+def test_against_the_plain_form(n, d, V, dtype):
+    h, W, labels, up = _data(n, d, V, dtype, seed=n + d + V)
+    _check(h, W, labels, "mean", up)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("reduction", ["sum", "none"])
+@pytest.mark.parametrize("n,d,V", [(3, 5, 7), (200, 96, 300), (1, 256, 4000), (1500, 24, 13)])
+def test_reductions(n, d, V, dtype, reduction):
+    h, W, labels, up = _data(n, d, V, dtype, seed=3)
+    _check(h, W, labels, reduction, up)
+    _check(h, W, labels, reduction, up * 1e-4)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,V", [(4, 8, 6), (300, 64, 500)])
+def test_rows_left_out(n, d, V, dtype):
+    h, W, labels, up = _data(n, d, V, dtype, seed=4)
+    # all of them: no loss and no gradient
+    none = torch.full_like(labels, -100)
+    hr, Wr = h.clone().requires_grad_(True), W.clone().requires_grad_(True)
+    for reduction in ("mean", "sum"):
+        loss = linear_cross_entropy(hr, Wr, none, reduction=reduction)
+        assert float(loss) == 0.0
+        for g in torch.autograd.grad(loss, (hr, Wr)):
+            assert bool((g == 0).all())
+    # what they hold counts for nothing, NaN and Inf included
+    labels[1] = -100
+    labels[0] = 1
+    clean = h.clone()
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        h[1] = bad
+        h[1, 0] = 0.0
+        want = api.ecc_xent_fwd(clean, W, labels)
+        got = api.ecc_xent_fwd(h, W, labels)
+        assert torch.equal(want[0], got[0]) and torch.equal(want[2], got[2])
+        one = torch.ones((), device="cuda")
+        for a, c in zip(api.ecc_xent_bwd(clean, W, labels, one, *want[1:]), api.ecc_xent_bwd(h, W, labels, one, *got[1:])):
+            assert torch.equal(a, c)
+    # another index for it, a class of its own
+    h = clean
+    _check(h, W, torch.where(labels == -100, 2, labels), "mean", up, ignore=2)
+    _check(h, W, labels.clamp_min(0), "mean", up, ignore=-1)
+
+
+def test_labels_out_of_range_are_seen():
+    h, W, labels, up = _data(40, 16, 30, F32, seed=5, ignored=0.0)
+    good = api.ecc_xent_fwd(h, W, labels, reduction="none")[0]
+    for bad in (-1, 30, 2 ** 40, -2 ** 60):
+        lab = labels.clone()
+        lab[7] = bad
+        loss, lse, counted = api.ecc_xent_fwd(h, W, lab, reduction="none")
+        assert bool(torch.isnan(loss[7])) and torch.equal(loss[:7], good[:7]) and torch.equal(loss[8:], good[8:])
+        dh, dW = api.ecc_xent_bwd(h, W, lab, torch.ones(40, device="cuda"), lse, counted, reduction="none")
+        assert bool(torch.isnan(dh[7]).all()) and bool(torch.isfinite(dh[:7]).all()) and bool(torch.isnan(dW).all())
+        assert bool(torch.isnan(api.ecc_xent_fwd(h, W, lab)[0]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_logits_do_not_overflow(dtype):
+    h, W, labels, up = _data(50, 32, 400, dtype, seed=6)
+    _check(h * 64, W * 16, labels, "mean", up)   # differences of thousands: one class has it all
+    low = W.clone()
+    low[5:] = 0
+    _check(h, low, labels % 5 + (labels < 0) * -100, "mean", up)
+
+
+def test_infinite_logits():
+    """A weight of -inf takes its class out of the sum; a logit of +inf or NaN leaves no finite loss."""
+    h = torch.ones(3, 4, device="cuda")
+    W = torch.randn(9, 4, device="cuda", generator=torch.Generator("cuda").manual_seed(0))
+    labels = torch.tensor([0, 1, 2], device="cuda")
+    gone = W.clone()
+    gone[8] = -float("inf")
+    want = api.ecc_xent_fwd(h, W[:8].contiguous(), labels, reduction="none")[0]
+    got = api.ecc_xent_fwd(h, gone, labels, reduction="none")[0]
+    assert float((want - got).abs().max()) < 1e-6
+    for bad in (float("inf"), float("nan")):
+        gone[8] = bad
+        assert not bool(torch.isfinite(api.ecc_xent_fwd(h, gone, labels, reduction="none")[0]).any())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_layouts(dtype):
+    h, W, labels, up = _data(24, 40, 50, dtype, seed=7)
+    want = linear_cross_entropy(h, W, labels, reduction="none")
+    assert torch.equal(linear_cross_entropy(h.view(2, 3, 4, 40), W, labels.view(2, 3, 4), reduction="none"), want.view(2, 3, 4))
+    assert torch.equal(linear_cross_entropy(h.t().contiguous().t(), W.t().contiguous().t(), labels, reduction="none"), want)
+    for shift in (1, 2, 3, 5):
+        room = torch.zeros(h.numel() + 8, dtype=dtype, device="cuda")
+        off = room[shift:shift + h.numel()].view_as(h)
+        off.copy_(h)
+        wroom = torch.zeros(W.numel() + 8, dtype=dtype, device="cuda")
+        woff = wroom[shift:shift + W.numel()].view_as(W)
+        woff.copy_(W)
+        _check(off, woff, labels, "mean", up)
+        # outputs off their alignment, nothing beside them touched
+        loss, lse, counted = api.ecc_xent_fwd(off, woff, labels)
+        gh = torch.full((h.numel() + 8,), 7.0, dtype=dtype, device="cuda")
+        gw = torch.full((W.numel() + 8,), 7.0, dtype=dtype, device="cuda")
+        api.ecc_xent_bwd(off, woff, labels, torch.ones((), device="cuda"), lse, counted,
+                         grad_hidden=gh[shift:shift + h.numel()].view_as(h), grad_weight=gw[shift:shift + W.numel()].view_as(W))
+        for t, size in ((gh, h.numel()), (gw, W.numel())):
+            assert bool((t[:shift] == 7).all()) and bool((t[shift + size:] == 7).all())
+
+
+@pytest.mark.parametrize("n,d,V,dtype", [(300, 64, 900, BF16), (40, 50, 3000, F32), (3000, 32, 20, F16)])
+def test_same_bits_again_and_one_gradient_alone(n, d, V, dtype):
+    h, W, labels, up = _data(n, d, V, dtype, seed=8)
+    loss, lse, counted = api.ecc_xent_fwd(h, W, labels)
+    assert int(counted) == int((labels != -100).sum())
+    one = torch.ones((), device="cuda")
+    dh, dW = api.ecc_xent_bwd(h, W, labels, one, lse, counted)
+    for _ in range(3):
+        again = api.ecc_xent_fwd(h, W, labels)
+        assert torch.equal(loss, again[0]) and torch.equal(lse, again[1])
+        a, c = api.ecc_xent_bwd(h, W, labels, one, lse, counted)
+        assert torch.equal(a, dh) and torch.equal(c, dW)
+    a, c = api.ecc_xent_bwd(h, W, labels, one, lse, counted, skip=("grad_weight",))
+    assert torch.equal(a, dh) and c is None
+    a, c = api.ecc_xent_bwd(h, W, labels, one, lse, counted, skip=("grad_hidden",))
+    assert a is None and torch.equal(c, dW)
+
+
+def test_gradient_against_differences():
+    h, W, labels, up = _data(5, 6, 9, F32, seed=9, ignored=0.0)
+    hr, Wr = h.clone().requires_grad_(True), W.clone().requires_grad_(True)
+    linear_cross_entropy(hr, Wr, labels).backward()
+    for t, grad, at in ((h, hr.grad, (2, 3)), (W, Wr.grad, (4, 1)), (W, Wr.grad, (int(labels[0]), 0))):
+        d = []
+        for sign in (1, -1):
+            z = t.double().clone()
+            z[at] += sign * 1e-4
+            args = (z, W.double()) if t is h else (h.double(), z)
+            d.append(float(torch.nn.functional.cross_entropy(args[0] @ args[1].t(), labels)))
+        assert abs((d[0] - d[1]) / 2e-4 - float(grad[at])) < 1e-5
+
+
+def test_module_and_no_rows():
+    head = LinearCrossEntropy(30, 12).cuda()
+    h = torch.randn(4, 5, 12, device="cuda", generator=torch.Generator("cuda").manual_seed(1), requires_grad=True)
+    labels = torch.arange(20, device="cuda").view(4, 5)
+    head(h, labels).backward()
+    assert head.weight.grad.shape == (30, 12) and h.grad.shape == h.shape
+    for reduction, shape in (("mean", ()), ("sum", ()), ("none", (0, 5))):
+        e = torch.zeros(0, 5, 12, device="cuda", requires_grad=True)
+        head.zero_grad()
+        loss = linear_cross_entropy(e, head.weight, labels[:0], reduction=reduction)
+        assert loss.shape == shape and loss.dtype == F32
+        loss.sum().backward()
+        assert e.grad.shape == e.shape and bool((head.weight.grad == 0).all())
+
+
+def test_on_a_stream_of_its_own_and_in_graphs():
+    h, W, labels, up = _data(300, 64, 2000, BF16, seed=10)
+    one = torch.ones((), device="cuda")
+
+    def step(hi):
+        loss, lse, counted = api.ecc_xent_fwd(hi, W, labels)
+        return (loss, *api.ecc_xent_bwd(hi, W, labels, one, lse, counted))
+    want = step(h)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = step(h)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(want, got))
+    ins = [h.clone(), h.clone()]
+    graphs, outs = [], []
+    for hi in ins:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(step(hi))
+        graphs.append(g)
+    side = torch.cuda.Stream()
+    for k in range(4):
+        for i, hi in enumerate(ins):
+            hi.copy_(_data(300, 64, 2000, BF16, seed=30 + 2 * k + i)[0])
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        with torch.cuda.stream(side):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        for hi, out in zip(ins, outs):
+            for a, c in zip(step(hi), out):
+                assert torch.equal(a, c)
+
+
+def test_refusals():
+    h, W, labels, up = _data(6, 8, 10, F32, seed=11)
+    for call in (lambda: linear_cross_entropy(h.cpu(), W, labels), lambda: linear_cross_entropy(h, W.half(), labels),
+                 lambda: linear_cross_entropy(h, W[:, :4], labels), lambda: linear_cross_entropy(h, W, labels[:3]),
+                 lambda: linear_cross_entropy(h, W, labels.int()), lambda: linear_cross_entropy(h, W, labels, reduction="max"),
+                 lambda: linear_cross_entropy(h.double(), W.double(), labels),
+                 lambda: api.ecc_xent_fwd(h.t().contiguous().t(), W, labels),
+                 lambda: api.ecc_xent_bwd(h, W, labels, torch.ones(6, device="cuda"), torch.zeros(6, device="cuda"),
+                                          torch.ones((), dtype=torch.int64, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(api.EccError) as e:
+        api.ecc_xent_fwd(h, W, labels, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == -3
