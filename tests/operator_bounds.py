@@ -33,8 +33,9 @@ def norm_reference(x, groups, w, b, eps, act, dy=None):
     xhat = dev * rstd
     v = xhat * w + b
     # the scale from squares summed in float32 (300 E of the variance, half of it in its root) and a few roundings, on
-    # differences that carry a rounding of their own
-    d_xhat = 160 * E * xhat.abs()
+    # differences that carry a rounding of their own; and the mean, from differences summed in float32 over runs of at most 128
+    # values: 4 sqrt(128) E = 45 E of the differences' mean size, which two values of one spread have at sqrt(2) spreads: 64 E
+    d_xhat = 160 * E * xhat.abs() + 64 * E
     d_v = d_xhat * w.abs() + 4 * E * (v.abs() + b.abs())
     sig = torch.sigmoid(v)
     y = {"none": v, "relu": v.clamp_min(0.0), "silu": v * sig}[act]
