@@ -10,8 +10,10 @@
 //
 // Two ways:
 //   fused   the points of some groups of one item fit one block's registers: one launch reads, sums, writes.
-//   swept   sums of blocks over runs of rows (partials in the workspace), a joining kernel, and a second sweep that writes.
-//           Items are taken in chunks that the Infinity Cache holds, so that the second sweep reads little from memory.
+//   swept   sums of blocks over runs of rows (partials in the workspace), a joining kernel, and a second sweep that writes,
+//           in the opposite order.  (Sweeping items in chunks that the Infinity Cache holds, so that the second sweep reads
+//           little from memory, costs more in short launches than it spares: step on 8 x 512^2 x 128 in bfloat16 1407 us in
+//           chunks of 128 MiB, 1077 in chunks of 256, 907 whole.)
 //
 // Squares are summed about a value of the data.  A thread takes its column's first value K and sums x - K and (x - K)^2 in
 // float32 over at most 128 rows: what cancels in q - s^2 / n is at most n times the squares about the mean, because K is one
@@ -87,28 +89,27 @@ struct NormLane {
   }
 };
 
-// Count, mean and squares of a group, joined by one wave.  Entries are [lanes][width], `per` to a thread, each standing for
-// `unit` values a row; those of the group are first .. first + len - 1 of every lane, and again at every `again` (rows that
-// hold the channels several times; 0: once).
+// Count, mean and squares of a group, joined by `team` lanes of a wave (a power of two).  Entries are [lanes][width], `per` to
+// a thread, each standing for `unit` values a row; those of the group are first .. first + len - 1 of every lane, and again at
+// every `again` (rows that hold the channels several times; 0: once).
 __device__ __forceinline__ Moments join_entries(const double* mean, const float* m2, const int* cnt, int wide, int lanes,
-                                                int width, int first, int len, int again, int per, int unit) {
-  const int lane = threadIdx.x & 63;
+                                                int width, int first, int len, int again, int per, int unit, int team) {
+  const int lane = threadIdx.x & (team - 1);
   const int repeats = again > 0 ? width / again : 1, row = repeats * len;
   double n = 0.0, s = 0.0;
-  for (int i = lane; i < lanes * row; i += 64) {
+  for (int i = lane; i < lanes * row; i += team) {
     const int rl = i / row, k = i - rl * row, at = (k / len) * again + first + k % len;
     const double c = (double)(cnt[rl * wide + at / per] * unit);
     n += c;
     if (c > 0.0) s += c * mean[rl * width + at];
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
+  for (int o = team / 2; o > 0; o >>= 1) {
     n += __shfl_xor(n, o);
     s += __shfl_xor(s, o);
   }
   const double mu = n > 0.0 ? s / n : 0.0;
   double q = 0.0;
-  for (int i = lane; i < lanes * row; i += 64) {
+  for (int i = lane; i < lanes * row; i += team) {
     const int rl = i / row, k = i - rl * row, at = (k / len) * again + first + k % len;
     const double c = (double)(cnt[rl * wide + at / per] * unit);
     if (c > 0.0) {
@@ -116,8 +117,7 @@ __device__ __forceinline__ Moments join_entries(const double* mean, const float*
       q += (double)m2[rl * width + at] + c * d * d;
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) q += __shfl_xor(q, o);
+  for (int o = team / 2; o > 0; o >>= 1) q += __shfl_xor(q, o);
   return {n, mu, q};
 }
 
@@ -153,46 +153,62 @@ struct Column {
   }
 };
 
-// The block's moments, group by group: `done(local group, Moments)` is called by every lane of one wave.  groups g0 .. g1 - 1
-// of the block's channels c0 .. (a slice, or a column range).  shared: entries [threads][V or 1].
+// values side by side in a vector that are sure to be of one group
+__host__ __device__ __forceinline__ int run_of(int Cg, int V) {
+  int run = 1;
+  while (run < V && Cg % (2 * run) == 0) run *= 2;
+  return run;
+}
+
+// The block's moments: `done(group, Moments)` is called by one thread for each group of the block's channels c0 .. cend - 1 (a
+// slice, or a column range).  shared: entries [threads][V / run].
 template <int V, typename F>
 __device__ __forceinline__ void block_moments(const Column<V>& col, const NormGeo& geo, const NormLane& l, int Cg, int c0, int cend,
                                               double* e_mean, float* e_m2, int* e_cnt, const F& done) {
   const int t = threadIdx.x;
-  const bool whole = Cg % V == 0;  // a vector's elements are of one group: one entry a thread
-  const int unit = whole ? V : 1, per = V / unit;
+  const int unit = run_of(Cg, V), per = V / unit;  // values of one group side by side: one entry for each such run
   if (t < geo.wide * geo.lanes) e_cnt[t] = l.on ? col.n : 0;
   if (l.on && col.n > 0) {
-    if (whole) {
-      double mu = 0.0;
+    double mu[V];
+    float m2[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) mu += col.mean(i);
-      mu *= 1.0 / V;
-      float m2 = 0.0f;
+    for (int i = 0; i < V; ++i) {
+      mu[i] = col.mean(i);
+      m2[i] = col.m2(i);
+    }
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float d = (float)(col.mean(i) - mu);
-        m2 += col.m2(i) + (float)col.n * d * d;
+    for (int step = 1; step < V; step *= 2) {  // runs of `step` values joined in pairs
+      if (step < unit) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2 * step) {
+          const float d = (float)(mu[i + step] - mu[i]);
+          m2[i] += m2[i + step] + 0.5f * (float)(col.n * step) * d * d;
+          mu[i] = 0.5 * (mu[i] + mu[i + step]);
+        }
       }
-      e_mean[t] = mu;
-      e_m2[t] = m2;
-    } else {
+    }
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        e_mean[t * V + i] = col.mean(i);
-        e_m2[t * V + i] = col.m2(i);
+    for (int i = 0; i < V; ++i) {
+      if (i % unit == 0) {
+        e_mean[t * per + i / unit] = mu[i];
+        e_m2[t * per + i / unit] = m2[i];
       }
     }
   }
   __syncthreads();
-  // entries of a lane: its columns in order, `per` each; channel c0 is entry 0
-  const int width = geo.wide * per, again = geo.channels / unit;
+  // entries of a lane: its columns in order, `per` each; channel c0 is entry 0.  Groups of few entries share a wave.
+  const int width = geo.wide * per, again = geo.passes > 1 ? 0 : geo.channels / unit;
   const int g0 = c0 / Cg, g1 = (cend - 1) / Cg;
-  for (int g = g0 + (t >> 6); g <= g1; g += (int)(blockDim.x >> 6)) {
+  const int most = geo.lanes * (again ? width / again : 1) * ((Cg + unit - 1) / unit);
+  int team = 64;
+  while (team > 1 && team / 2 >= most) team /= 2;
+  const int teams = (int)blockDim.x / team;
+  for (int gb = g0; gb <= g1; gb += teams) {  // (whole waves take part: a team without a group repeats the last one's)
+    const int g = min(gb + t / team, g1);
     const int lo = max(g * Cg, c0), hi = min((g + 1) * Cg, cend);
-    const Moments m = join_entries(e_mean, e_m2, e_cnt, geo.wide, geo.lanes, width, (lo - c0) / unit, (hi - lo) / unit,
-                             geo.passes > 1 ? 0 : again, per, unit);
-    done(g, m);
+    const Moments m = join_entries(e_mean, e_m2, e_cnt, geo.wide, geo.lanes, width, (lo - c0) / unit, (hi - lo) / unit, again, per,
+                                   unit, team);
+    if ((t & (team - 1)) == 0 && gb + t / team <= g1) done(g, m);
   }
 }
 
@@ -230,7 +246,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_stats_kernel(NormArgs a, No
     }
   }
   double* e_mean = reinterpret_cast<double*>(smem);
-  const int per = Cg % V == 0 ? 1 : V, entries = geo.wide * geo.lanes * per;
+  const int per = V / run_of(Cg, V), entries = geo.wide * geo.lanes * per;
   float* e_m2 = reinterpret_cast<float*>(e_mean + entries);
   int* e_cnt = reinterpret_cast<int*>(e_m2 + entries);
   const int c0 = geo.passes > 1 ? z * geo.wide * V : 0, cend = geo.passes > 1 ? min(a.C, c0 + geo.wide * V) : a.C;
@@ -241,35 +257,48 @@ __global__ __launch_bounds__(kNormThreads) void norm_stats_kernel(NormArgs a, No
       if (g < c0 / Cg || g > (cend - 1) / Cg) out[(int64_t)g * nq + q] = {0.0, 0.0, 0.0};
   }
   block_moments(col, geo, l, Cg, c0, cend, e_mean, e_m2, e_cnt, [&](int g, const Moments& m) {
-    if ((threadIdx.x & 63) == 0) out[(int64_t)g * nq + q] = m;
+    out[(int64_t)g * nq + q] = m;
   });
 }
 
-// a wave for each item and group
-__global__ __launch_bounds__(256) void norm_join_kernel(const Moments* part, int64_t groups, int nq, float eps, double* stats) {
-  const int64_t g = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (g >= groups) return;
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ void block_add(double& u, double& v, double (*room)[2]) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    u += __shfl_xor(u, o);
+    v += __shfl_xor(v, o);
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+    room[threadIdx.x >> 6][0] = u;
+    room[threadIdx.x >> 6][1] = v;
+  }
+  __syncthreads();
+  u = v = 0.0;
+  for (int k = 0; k < (int)(blockDim.x >> 6); ++k) {
+    u += room[k][0];
+    v += room[k][1];
+  }
+}
+
+// a block for each item and group
+__global__ __launch_bounds__(256) void norm_join_kernel(const Moments* part, int nq, float eps, double* stats) {
+  __shared__ double room[4][2];
+  const int64_t g = blockIdx.x;
   const Moments* m = part + g * nq;
   double n = 0.0, s = 0.0;
-  for (int i = lane; i < nq; i += 64) {
+  for (int i = threadIdx.x; i < nq; i += 256) {
     n += m[i].n;
     s += m[i].n * m[i].mean;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    n += __shfl_xor(n, o);
-    s += __shfl_xor(s, o);
-  }
+  block_add(n, s, room);
   const double mu = s / n;
-  double q = 0.0;
-  for (int i = lane; i < nq; i += 64) {
+  double q = 0.0, zero = 0.0;
+  for (int i = threadIdx.x; i < nq; i += 256) {
     const double d = m[i].mean - mu;
     q += m[i].m2 + m[i].n * d * d;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) q += __shfl_xor(q, o);
-  if (lane == 0) {
+  block_add(q, zero, room);
+  if (threadIdx.x == 0) {
     stats[g * 2] = mu;
     stats[g * 2 + 1] = 1.0 / sqrt(q / n + (double)eps);
   }
@@ -303,7 +332,7 @@ __device__ __forceinline__ void over_rows(const NormGeo& geo, const NormLane& l,
 // ---- swept: second sweep of the forward pass ---------------------------------------------------------------------------
 template <typename T, int V>
 __global__ __launch_bounds__(kNormThreads) void norm_apply_kernel(NormArgs a, NormGeo geo, int64_t n0, const double* stats) {
-  const int64_t block = blockIdx.x;
+  const int64_t block = gridDim.x - 1 - blockIdx.x;  // (what the first sweep read last is still in the caches)
   const int p = (int)(block % geo.parts), z = (int)(block / geo.parts % geo.passes);
   const int64_t n = n0 + block / geo.parts / geo.passes;
   const NormLane l(geo, z);
@@ -477,7 +506,7 @@ __global__ __launch_bounds__(kJoinThreads) void norm_params_kernel(NormArgs a, c
 // (1/m) sum w dv and (1/m) sum w dv xhat of every group of items n0 ..: a block each
 __global__ __launch_bounds__(kJoinThreads) void norm_groups_kernel(NormArgs a, const float* part, int parts, int64_t n0,
                                                                    double* m12) {
-  __shared__ double room[2][kJoinThreads / 64];
+  __shared__ double room[kJoinThreads / 64][2];
   const int Cg = a.C / a.G, g = (int)(blockIdx.x % a.G);
   const int64_t n = n0 + blockIdx.x / a.G;
   const float* p = part + n * parts * 2 * a.C + (int64_t)g * Cg;
@@ -490,22 +519,8 @@ __global__ __launch_bounds__(kJoinThreads) void norm_groups_kernel(NormArgs a, c
     s1 += w * (double)p[r * 2 * a.C + c];
     s2 += w * (double)p[(r * 2 + 1) * a.C + c];
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    s1 += __shfl_xor(s1, o);
-    s2 += __shfl_xor(s2, o);
-  }
-  if ((threadIdx.x & 63) == 0) {
-    room[0][threadIdx.x >> 6] = s1;
-    room[1][threadIdx.x >> 6] = s2;
-  }
-  __syncthreads();
+  block_add(s1, s2, room);
   if (threadIdx.x == 0) {
-    s1 = s2 = 0.0;
-    for (int k = 0; k < kJoinThreads / 64; ++k) {
-      s1 += room[0][k];
-      s2 += room[1][k];
-    }
     const double m = (double)a.points * Cg;
     m12[(n * a.G + g) * 2] = s1 / m;
     m12[(n * a.G + g) * 2 + 1] = s2 / m;
@@ -538,7 +553,7 @@ __device__ __forceinline__ void put_dx(const Scale<V>& sc, const Slopes<V>& sl, 
 // ---- swept: second sweep of the backward pass --------------------------------------------------------------------------
 template <typename T, int V>
 __global__ __launch_bounds__(kNormThreads) void norm_dx_kernel(NormArgs a, NormGeo geo, int64_t n0, const double* m12) {
-  const int64_t block = blockIdx.x;
+  const int64_t block = gridDim.x - 1 - blockIdx.x;  // (what the first sweep read last is still in the caches)
   const int p = (int)(block % geo.parts), z = (int)(block / geo.parts % geo.passes);
   const int64_t n = n0 + block / geo.parts / geo.passes;
   const NormLane l(geo, z);
@@ -600,21 +615,19 @@ __global__ __launch_bounds__(kNormFused) void norm_fused_kernel(NormArgs a, Norm
       else col.add(keep[k]);
     }
   }
-  const int per = Cg % V == 0 ? 1 : V, entries = geo.wide * geo.lanes * per;
+  const int per = V / run_of(Cg, V), entries = geo.wide * geo.lanes * per;
   double* gm = reinterpret_cast<double*>(smem);  // [gc][2]
   double* e_mean = gm + 2 * gc;
   float* e_m2 = reinterpret_cast<float*>(e_mean + entries);
   int* e_cnt = reinterpret_cast<int*>(e_m2 + entries);
   block_moments(col, geo, l, Cg, 0, geo.channels, e_mean, e_m2, e_cnt, [&](int g, const Moments& m) {
-    if ((threadIdx.x & 63) == 0) {
-      const double rstd = 1.0 / sqrt(m.m2 / m.n + (double)a.eps);
-      gm[g * 2] = m.mean;
-      gm[g * 2 + 1] = rstd;
-      if (a.stats) {
-        double* st = a.stats + (n * a.G + c0 / Cg + g) * 2;
-        st[0] = m.mean;
-        st[1] = rstd;
-      }
+    const double rstd = 1.0 / sqrt(m.m2 / m.n + (double)a.eps);
+    gm[g * 2] = m.mean;
+    gm[g * 2 + 1] = rstd;
+    if (a.stats) {
+      double* st = a.stats + (n * a.G + c0 / Cg + g) * 2;
+      st[0] = m.mean;
+      st[1] = rstd;
     }
   });
   __syncthreads();
@@ -731,8 +744,7 @@ __global__ __launch_bounds__(kNormFused) void norm_fused_bwd_kernel(NormArgs a, 
 }
 
 // ---- plans ---------------------------------------------------------------------------------------------------------------
-constexpr int64_t kNormBlocks = 2048;                   // of a sweep over everything, about
-constexpr int64_t kNormChunk = (int64_t)128 << 20;      // bytes of a chunk of items (both inputs of the backward pass)
+constexpr int64_t kNormBlocks = 1024;  // of a sweep, about: what the card holds at a time (2048: 924 us for 907, above)
 
 // elements a vector may have: 16 bytes' worth, or fewer where an item's size or an address does not allow it
 static int norm_vector(const NormArgs& a, int size) {
@@ -754,14 +766,9 @@ static void share_rows(NormGeo& g, int64_t items) {
   g.parts = (int)((g.rows + g.per - 1) / g.per);
 }
 
-// items of a chunk: of `bytes` a value read
-static int64_t norm_chunk(const NormArgs& a, int bytes) {
-  return std::max<int64_t>(1, std::min(a.batch, kNormChunk / std::max<int64_t>(1, a.points * a.C * bytes)));
-}
-
 // Columns: rows of lcm(C, V) elements where a block can hold them; else V divides C, and blocks take ranges of columns that
 // hold whole groups, or (groups wider than a block) any.
-static NormGeo norm_geo(const NormArgs& a, int& V, int bytes) {
+static NormGeo norm_geo(const NormArgs& a, int& V) {
   NormGeo g{};
   const int Cg = a.C / a.G;
   g.channels = a.C;
@@ -785,13 +792,13 @@ static NormGeo norm_geo(const NormArgs& a, int& V, int bytes) {
   g.stride = row;
   g.vectors = a.points * a.C / V;
   g.rows = (g.vectors + g.cols - 1) / g.cols;
-  share_rows(g, norm_chunk(a, bytes));
+  share_rows(g, a.batch);
   return g;
 }
 
 // Slices for the fused kernels: as many groups as fit, fewer where that gives the card more blocks without cutting a row into
 // runs of less than 64 bytes.  K: vectors a thread keeps (0: no slice fits).
-static size_t moments_room(int threads, int Cg, int V) { return (size_t)threads * ((Cg % V ? V : 1) * 12 + 4); }
+static size_t moments_room(int threads, int Cg, int V) { return (size_t)threads * (V / run_of(Cg, V) * 12 + 4); }
 static size_t columns_room(const NormGeo& g, int V) {
   return (size_t)std::max(g.wide * ((g.lanes + 1) / 2), g.wide) * 2 * V * sizeof(float);
 }
@@ -831,17 +838,15 @@ static int norm_fused_plan(const NormArgs& a, int V, int size, int most, NormGeo
 
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 static unsigned waves(int threads) { return (unsigned)((threads + 63) / 64 * 64); }
-// Room for either way with any vector and chunk: partial moments or sums, then two doubles a group of every item.
+// Room for either way with any vector: partial moments or sums, then two doubles a group of every item.
 static size_t norm_partials(const NormArgs& a) {
   size_t most = 256;
   for (int V = 1; V <= 8; V *= 2) {
     if (a.points * a.C % V) continue;
-    for (int bytes = 2; bytes <= 8; bytes *= 2) {
-      int v = V;
-      const NormGeo g = norm_geo(a, v, bytes);
-      const size_t nq = (size_t)g.parts * (g.across ? g.passes : 1);
-      most = std::max(most, std::max((size_t)a.batch * a.G * nq * sizeof(Moments), (size_t)a.batch * g.parts * 2 * a.C * sizeof(float)));
-    }
+    int v = V;
+    const NormGeo g = norm_geo(a, v);
+    const size_t nq = (size_t)g.parts * (g.across ? g.passes : 1);
+    most = std::max(most, std::max((size_t)a.batch * a.G * nq * sizeof(Moments), (size_t)a.batch * g.parts * 2 * a.C * sizeof(float)));
   }
   return align256(most);
 }
@@ -877,18 +882,17 @@ static hipError_t norm_fwd_v(const NormArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   int v = V;
-  const NormGeo g = norm_geo(a, v, sizeof(T));
+  const NormGeo g = norm_geo(a, v);
   const unsigned threads = waves(g.wide * g.lanes);
   const int nq = g.parts * (g.across ? g.passes : 1);
   Moments* part = static_cast<Moments*>(a.ws);
   double* stats = a.stats ? a.stats : reinterpret_cast<double*>(static_cast<char*>(a.ws) + norm_partials(a));
-  const int64_t each = std::min(norm_chunk(a, sizeof(T)), norm_launch(a.batch, (int64_t)g.parts * g.passes, threads));
+  const int64_t each = norm_launch(a.batch, (int64_t)g.parts * g.passes, threads);
   for (int64_t n0 = 0; n0 < a.batch; n0 += each) {
     const int64_t items = std::min(each, a.batch - n0);
     const dim3 grid((unsigned)(items * g.parts * g.passes));
     hipLaunchKernelGGL((norm_stats_kernel<T, V>), grid, dim3(threads), moments_room(g.wide * g.lanes, Cg, V), st, a, g, n0, part);
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((items * a.G + 3) / 4)), dim3(256), 0, st, part, items * a.G, nq, a.eps,
-                       stats + n0 * a.G * 2);
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(items * a.G)), dim3(256), 0, st, part, nq, a.eps, stats + n0 * a.G * 2);
     hipLaunchKernelGGL((norm_apply_kernel<T, V>), grid, dim3(threads), 0, st, a, g, n0, stats);
   }
   return hipGetLastError();
@@ -920,10 +924,10 @@ static hipError_t norm_bwd_v(const NormArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   int v = V;
-  const NormGeo g = norm_geo(a, v, 2 * sizeof(T));
+  const NormGeo g = norm_geo(a, v);
   const unsigned threads = waves(g.wide * g.lanes);
   double* m12 = reinterpret_cast<double*>(static_cast<char*>(a.ws) + norm_partials(a));
-  const int64_t each = std::min(norm_chunk(a, 2 * sizeof(T)), norm_launch(a.batch, (int64_t)g.parts * g.passes, threads));
+  const int64_t each = norm_launch(a.batch, (int64_t)g.parts * g.passes, threads);
   for (int64_t n0 = 0; n0 < a.batch; n0 += each) {
     const int64_t items = std::min(each, a.batch - n0);
     const dim3 grid((unsigned)(items * g.parts * g.passes));
@@ -941,7 +945,7 @@ static hipError_t norm_bwd_v(const NormArgs& a, hipStream_t st) {
 template <typename T, bool BWD>
 static hipError_t norm_go(const NormArgs& a, hipStream_t st) {
   int V = norm_vector(a, sizeof(T));
-  norm_geo(a, V, sizeof(T));
+  norm_geo(a, V);
 #define ECC_GO(VV) return BWD ? norm_bwd_v<T, VV>(a, st) : norm_fwd_v<T, VV>(a, st)
   if (V == 1) ECC_GO(1);
   if (V == 2) ECC_GO(2);
