@@ -1,220 +1,392 @@
 // Softmax cross entropy of a linear head, in pieces of the classes:
 //   z_iv = <h_i, W_v>,   lse_i = log sum_v exp z_iv,   loss_i = lse_i - z_{i,label},
 //   dz_iv = (exp(z_iv - lse_i) - [v = label_i]) g_i,   dh = dz W,   dW = dz^T h.
-// The logits are never kept: the forward pass leaves a maximum and a sum for each row and piece, the backward pass forms
-// dz of one piece at a time.
+// The logits are never kept: the forward pass leaves a maximum and a sum for each row and tile of classes, the backward pass
+// forms dz of one piece of the classes at a time, in the operands' type, for the two products that read it.
+//
+// Matrix products bound it (ecc_xent_product.h): rows x dim x classes multiply-adds forward, three times that backward.
 #include "ecc_xent.h"
 
 #include <algorithm>
 
+#include "ecc_xent_product.h"
+
 namespace ecc {
 
-constexpr int kTile = 64, kDeep = 16;          // a block's tile of a product and its steps along the summed axis
-constexpr int64_t kPieceBytes = (int64_t)64 << 20;
+// float16 holds dz as a multiple of 2^-14 of the largest upstream gradient: the probabilities of a large vocabulary are far below
+// its least number otherwise.  (They are at most 1: 2^14 is in range, and what is below 2^-28 of the largest loses digits.)
+constexpr float kHalfScale = 16384.0f;
 
-// acc[i][j] += sum_k a(m0 + ty 4 + i, k) b(k, n0 + tx 4 + j) for 16 x 16 threads; a and b give 0 outside
-template <typename A, typename B>
-__device__ __forceinline__ void tile_product(const A& a, const B& b, int64_t m0, int64_t n0, int64_t K, float (&acc)[4][4]) {
-  __shared__ float as[kDeep][kTile + 1], bs[kDeep][kTile + 1];
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  for (int64_t k0 = 0; k0 < K; k0 += kDeep) {
-    for (int e = tid; e < kDeep * kTile; e += 256) {
-      const int k = e % kDeep, i = e / kDeep;
-      as[k][i] = k0 + k < K ? a(m0 + i, k0 + k) : 0.0f;
-      bs[k][i] = k0 + k < K ? b(k0 + k, n0 + i) : 0.0f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kDeep; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(as[k][ty * 4 + i], bs[k][tx * 4 + j], acc[i][j]);
-    __syncthreads();
-  }
-}
+static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+static int64_t up_to(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 
-// (m, s) stands for s exp(m); a sum of exponentials under a running maximum
-__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
-  const float top = fmaxf(m, m2);
-  if (top == -INFINITY) return;
-  s = s * __expf(m - top) + s2 * __expf(m2 - top);
-  m = top;
-}
-
-// piece sums: part[row][tile] = (maximum, sum), and the label's logit
+// ---- operands --------------------------------------------------------------------------------------------------------------
+// rows of `dim` elements laid out as the products take them: [planes][rows][ld], zeros behind a row's end
 template <typename T>
-__global__ __launch_bounds__(256) void xent_sums_kernel(XentArgs a, float2* part, float* picked, int64_t tiles) {
-  const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
-  tile_product([&](int64_t m, int64_t k) { return m < a.rows ? widen(h[m * a.dim + k]) : 0.0f; },
-               [&](int64_t k, int64_t n) { return n < a.classes ? widen(w[n * a.dim + k]) : 0.0f; }, m0, n0, a.dim, acc);
-  for (int i = 0; i < 4; ++i) {
-    const int64_t row = m0 + ty * 4 + i;
-    float m = -INFINITY, s = 0.0f;
-    const int64_t label = row < a.rows ? a.labels[row] : -1;
-    for (int j = 0; j < 4; ++j) {
-      const int64_t v = n0 + tx * 4 + j;
-      if (v >= a.classes) continue;
-      if (acc[i][j] != acc[i][j]) { m = INFINITY; s = NAN; }
-      else join(m, s, acc[i][j], 1.0f);
-      if (v == label && row < a.rows) picked[row] = acc[i][j];
-    }
-    for (int o = 8; o > 0; o >>= 1) {
-      const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o);
-      join(m, s, m2, s2);
-    }
-    if (tx == 0 && row < a.rows) part[row * tiles + blockIdx.x] = make_float2(m, s);
+__global__ __launch_bounds__(256) void xent_lay_kernel(const T* __restrict__ from, int64_t rows, int dim, int ld,
+                                                       unsigned short* __restrict__ to) {
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, all = rows * ld;
+  if (at >= all) return;
+  const int64_t row = at / ld;
+  const int k = (int)(at - row * ld);
+  unsigned short s[8][3];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (sizeof(T) == 4) split3(k + i < dim ? widen(from[row * dim + k + i]) : 0.0f, s[i]);
+    else s[i][0] = k + i < dim ? reinterpret_cast<const unsigned short*>(from)[row * dim + k + i] : 0;
+  }
+#pragma unroll
+  for (int p = 0; p < (sizeof(T) == 4 ? 3 : 1); ++p) {
+    uint4 w;
+    w.x = (unsigned)s[0][p] | (unsigned)s[1][p] << 16;
+    w.y = (unsigned)s[2][p] | (unsigned)s[3][p] << 16;
+    w.z = (unsigned)s[4][p] | (unsigned)s[5][p] << 16;
+    w.w = (unsigned)s[6][p] | (unsigned)s[7][p] << 16;
+    *reinterpret_cast<uint4*>(to + p * all + at) = w;
   }
 }
 
-// a row's pieces joined: lse and the row's loss
-__global__ __launch_bounds__(64) void xent_rows_kernel(XentArgs a, const float2* part, const float* picked, float* each,
-                                                       int64_t tiles) {
-  const int64_t row = blockIdx.x;
+// ---- rows ------------------------------------------------------------------------------------------------------------------
+// A row's tiles joined by `team` lanes (a power of two): lse, and the row's loss.
+__global__ __launch_bounds__(256) void xent_rows_kernel(XentArgs a, const float2* part, const float* picked, float* each,
+                                                        int64_t parts, int team) {
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / team;
+  const int lane = threadIdx.x & (team - 1);
+  const bool in = row < a.rows;  // (whole waves take part in the exchanges)
+  const float2* p = part + (in ? row : 0) * parts;
   float m = -INFINITY;
-  for (int64_t t = threadIdx.x; t < tiles; t += 64) m = fmaxf(m, part[row * tiles + t].x);
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  for (int64_t t = lane; t < parts; t += team) m = fmaxf(m, p[t].x);
+  for (int o = team / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   double s = 0.0;
-  for (int64_t t = threadIdx.x; t < tiles; t += 64) {
-    const float2 p = part[row * tiles + t];
-    s += (double)p.y * (p.x == m ? 1.0 : (double)__expf(p.x - m));
-  }
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if (threadIdx.x != 0) return;
+  for (int64_t t = lane; t < parts; t += team) s += (double)p[t].y * (p[t].x == m ? 1.0 : (double)__expf(p[t].x - m));
+  for (int o = team / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if (!in || lane != 0) return;
   const double lse = (double)m + log(s);
   if (a.lse) a.lse[row] = (float)lse;
   const int64_t label = a.labels[row];
   each[row] = label == a.ignore ? 0.0f : label < 0 || label >= a.classes ? NAN : (float)(lse - (double)picked[row]);
 }
 
-__global__ __launch_bounds__(256) void xent_mean_kernel(XentArgs a, const float* each) {
-  __shared__ double part[256];
-  __shared__ int64_t cnt[256];
-  double s = 0.0;
-  int64_t n = 0;
-  for (int64_t i = threadIdx.x; i < a.rows; i += 256) {
-    s += (double)each[i];
-    n += a.labels[i] != a.ignore;
-  }
-  part[threadIdx.x] = s;
-  cnt[threadIdx.x] = n;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int k = 1; k < 256; ++k) { s += part[k]; n += cnt[k]; }
+// Sum of the rows' losses and their count, a run of rows a block; one block: the loss itself.
+struct RowSum { double sum; long long count; };
+constexpr int kSumThreads = 1024;
+
+__device__ __forceinline__ void xent_finish(const XentArgs& a, double s, long long n) {
   if (a.counted) a.counted[0] = n;
   if (a.reduction != kEach) a.loss[0] = (float)(a.reduction == kMean ? s / (double)(n > 0 ? n : 1) : s);
 }
-
-// dz of the classes v0 .. v0 + count
-template <typename T>
-__global__ __launch_bounds__(256) void xent_dz_kernel(XentArgs a, float* dz, int64_t v0, int64_t count) {
-  const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = v0 + (int64_t)blockIdx.x * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
-  tile_product([&](int64_t m, int64_t k) { return m < a.rows ? widen(h[m * a.dim + k]) : 0.0f; },
-               [&](int64_t k, int64_t n) { return n < a.classes ? widen(w[n * a.dim + k]) : 0.0f; }, m0, n0, a.dim, acc);
-  for (int i = 0; i < 4; ++i) {
-    const int64_t row = m0 + ty * 4 + i;
-    if (row >= a.rows) continue;
-    const int64_t label = a.labels[row];
-    float g = a.reduction == kEach ? a.up[row] : a.up[0];
-    if (a.reduction == kMean) g /= (float)(a.counted[0] > 0 ? a.counted[0] : 1);
-    if (label != a.ignore && (label < 0 || label >= a.classes)) g = NAN;
-    for (int j = 0; j < 4; ++j) {
-      const int64_t v = n0 + tx * 4 + j;
-      if (v >= v0 + count) continue;
-      const float p = __expf(acc[i][j] - a.lse[row]) - (v == label ? 1.0f : 0.0f);
-      dz[row * count + (v - v0)] = label == a.ignore ? 0.0f : p * g;
+__global__ __launch_bounds__(kSumThreads) void xent_sum_kernel(XentArgs a, const float* each, int64_t per, RowSum* out) {
+  __shared__ double sum[kSumThreads];
+  __shared__ long long count[kSumThreads];
+  const int t = threadIdx.x;
+  double s = 0.0;
+  long long n = 0;
+  const int64_t end = min(a.rows, (int64_t)(blockIdx.x + 1) * per);
+#pragma unroll 4
+  for (int64_t i = (int64_t)blockIdx.x * per + t; i < end; i += kSumThreads) {
+    s += (double)each[i];
+    n += a.labels[i] != a.ignore;
+  }
+  sum[t] = s;
+  count[t] = n;
+  __syncthreads();
+  for (int o = kSumThreads / 2; o > 0; o >>= 1) {
+    if (t < o) {
+      sum[t] += sum[t + o];
+      count[t] += count[t + o];
     }
+    __syncthreads();
+  }
+  if (t != 0) return;
+  if (gridDim.x == 1) xent_finish(a, sum[0], count[0]);
+  else out[blockIdx.x] = {sum[0], count[0]};
+}
+__global__ __launch_bounds__(64) void xent_total_kernel(XentArgs a, const RowSum* part, int blocks) {
+  double s = 0.0;
+  long long n = 0;
+  for (int k = threadIdx.x; k < blocks; k += 64) {
+    s += part[k].sum;
+    n += part[k].count;
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    s += __shfl_xor(s, o);
+    n += __shfl_xor(n, o);
+  }
+  if (threadIdx.x == 0) xent_finish(a, s, n);
+}
+
+// the largest |upstream gradient|, in one block: only where float16 meets a gradient for each row
+__global__ __launch_bounds__(kSumThreads) void xent_top_kernel(const float* up, int64_t rows, float* top) {
+  __shared__ float part[kSumThreads / 64];
+  float m = 0.0f;
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < rows; i += kSumThreads) m = fmaxf(m, fabsf(up[i]));
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int k = 0; k < kSumThreads / 64; ++k) m = fmaxf(m, part[k]);
+  top[0] = m;
+}
+
+// What each row's dz is multiplied by, which rows count, and what the products are multiplied by.
+__global__ __launch_bounds__(256) void xent_scale_kernel(XentArgs a, bool half, const float* top, float* row_scale,
+                                                         unsigned long long* keep, float* scale) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  float by = half ? kHalfScale : 1.0f, back = 1.0f / by;
+  if (a.reduction == kEach) {
+    if (half) {
+      const float t = top[0] > 0.0f ? top[0] : 1.0f;
+      by /= t;
+      back *= t;
+    }
+  } else {
+    back *= a.up[0];
+    if (a.reduction == kMean) back /= (float)(a.counted[0] > 0 ? a.counted[0] : 1);
+  }
+  bool counts = false;
+  if (i < a.rows) {
+    const int64_t label = a.labels[i];
+    counts = label != a.ignore;
+    float v = a.reduction == kEach ? a.up[i] * by : by;
+    if (counts && (label < 0 || label >= a.classes)) v = NAN;
+    row_scale[i] = v;
+  }
+  const unsigned long long bits = __ballot(counts);
+  if ((threadIdx.x & 63) == 0 && i < a.rows) keep[i / 64] = bits;
+  if (i == 0) scale[0] = back;
+}
+
+// out = narrow(scale * sum of the splits)
+template <typename O>
+__global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int splits, int64_t n, const float* scale, O* out) {
+  const float by = *scale;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    float s = sums[i];
+    for (int k = 1; k < splits; ++k) s += sums[k * n + i];
+    out[i] = narrow<O>(s * by);
   }
 }
 
-// dh (+)= dz W of a piece, summed in float32 over the pieces
+// ---- plans -----------------------------------------------------------------------------------------------------------------
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of dz, and of laid-out weights: what the Infinity Cache holds
+constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
+constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
+
+static int planes_of(int dtype) { return dtype == kF32 ? 3 : 1; }
+static int ld_of(int dim) { return (int)up_to(dim, 8); }
+
+// Tiles of 256 x 256 where they fill the card (one block a CU), of 128 x 128 otherwise; thin products have thin tiles.
+static int shape_of(int64_t M, int64_t N, int64_t runs) {
+  if (N <= 32) return 2;
+  if (M <= 32) return 3;
+  const int64_t large = (M + 255) / 256 * ((N + 255) / 256);
+  return M > 128 && N > 128 && large * runs >= 256 ? 0 : 1;
+}
+// The summed axis in runs, so that blocks fill the card: eight tiles a run or more, results within kSumsBytes.
+static int splits_of(int64_t M, int64_t N, int64_t K, int shape) {
+  const ProductPlan& p = kPlans[shape];
+  const int64_t blocks = (M + p.bm - 1) / p.bm * ((N + p.bn - 1) / p.bn), total = (K + kDepth - 1) / kDepth;
+  const int64_t fill = shape == 0 ? 256 : shape == 1 ? 512 : 1024;
+  int64_t want = std::min(std::max<int64_t>(1, fill / blocks), std::max<int64_t>(1, total / 8));
+  want = std::max<int64_t>(1, std::min(want, kSumsBytes / (M * N * 4)));
+  const int64_t steps = (total + want - 1) / want;
+  return (int)((total + steps - 1) / steps);
+}
+
+struct XentPlan {
+  int64_t fwd_piece, piece, ld_dz;
+  int fwd_shape, shape, hidden_shape, hidden_splits, weight_shape, weight_splits;
+  int64_t parts;
+  bool hidden_sums;
+  size_t lay_h, lay_w, lay_w_fwd;                        // bytes of laid-out operands
+  size_t part, picked, each, row_sums;                   // forward
+  size_t dz, sums_h, sums_w, row_scale, keep, scalars;   // backward
+};
+
+static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
+  XentPlan p{};
+  const int P = planes_of(dtype);
+  const int64_t ld = ld_of(dim);
+  const auto pieces = [&](int64_t most) {  // equal pieces of multiples of 256 classes, at most `most`
+    most = std::max<int64_t>(256, most / 256 * 256);
+    const int64_t count = (classes + most - 1) / most;
+    return std::min(classes, up_to((classes + count - 1) / count, 256));
+  };
+  p.fwd_shape = shape_of(classes, rows, 1);
+  p.parts = (classes + kPlans[p.fwd_shape].bm - 1) / kPlans[p.fwd_shape].bm * kPlans[p.fwd_shape].wm;
+  p.fwd_piece = pieces(std::min(kPieceMost * 8, kPieceBytes / (ld * 2 * P)));
+  p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * 2 * P), dtype == kF32 ? kPieceBytes / (ld * 2 * P) : kPieceMost}));
+  p.ld_dz = up_to(p.piece, 8);
+  p.shape = shape_of(p.piece, rows, 1);
+  const int64_t long_k = std::max<int64_t>(1, p.piece / kDepth / 16), long_n = std::max<int64_t>(1, rows / kDepth / 16);
+  p.hidden_shape = shape_of(dim, rows, long_k);
+  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape);
+  p.hidden_sums = p.hidden_splits > 1 || p.piece < classes;
+  p.weight_shape = shape_of(dim, p.piece, long_n);
+  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape);
+  p.lay_h = align256((size_t)rows * ld * 2 * P);
+  p.lay_w = align256((size_t)p.piece * ld * 2 * P);
+  p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * 2 * P);
+  p.part = align256((size_t)rows * p.parts * sizeof(float2));
+  p.picked = p.each = align256((size_t)rows * 4);
+  p.row_sums = align256(256 * sizeof(RowSum));
+  p.dz = align256((size_t)rows * p.ld_dz * 2 * P);
+  p.sums_h = p.hidden_sums ? align256((size_t)p.hidden_splits * rows * dim * 4) : 0;
+  p.sums_w = p.weight_splits > 1 ? align256((size_t)p.weight_splits * p.piece * dim * 4) : 0;
+  p.row_scale = align256((size_t)rows * 4);
+  p.keep = align256((size_t)(rows + 63) / 64 * 8);
+  p.scalars = 256;
+  return p;
+}
+
+size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int dtype, bool backward) {
+  const XentPlan p = xent_plan(rows, dim, classes, dtype);
+  if (!backward) return p.lay_h + p.lay_w_fwd + p.part + p.picked + p.each + p.row_sums;
+  return p.lay_h + p.lay_w + p.dz + p.sums_h + p.sums_w + p.row_scale + p.keep + p.scalars;
+}
+
+struct Room {  // hands out a workspace
+  char* at;
+  void* take(size_t n) {
+    void* p = at;
+    at += n;
+    return p;
+  }
+};
+
+// Whether the products can read the caller's own memory: 16-bit elements, rows of whole 16-byte chunks.
+static bool as_it_is(const void* p, int dim, int dtype) { return dtype != kF32 && dim % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
 template <typename T>
-__global__ __launch_bounds__(256) void xent_dh_kernel(XentArgs a, const float* dz, float* sum, int64_t v0, int64_t count) {
-  const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  const T* w = static_cast<const T*>(a.w);
-  tile_product([&](int64_t m, int64_t k) { return m < a.rows ? dz[m * count + k] : 0.0f; },
-               [&](int64_t k, int64_t n) { return n < a.dim ? widen(w[(v0 + k) * a.dim + n]) : 0.0f; }, m0, n0, count, acc);
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t row = m0 + ty * 4 + i, k = n0 + tx * 4 + j;
-      if (row >= a.rows || k >= a.dim) continue;
-      const float v = acc[i][j] + (v0 > 0 ? sum[row * a.dim + k] : 0.0f);
-      sum[row * a.dim + k] = v;
-      if (v0 + count >= a.classes) static_cast<T*>(a.dh)[row * a.dim + k] = narrow<T>(v);
-    }
+static Matrix laid(const T* from, int64_t rows, int dim, void* room, bool own, hipStream_t st) {
+  if (own) return {from, rows, dim, 0};
+  const int ld = ld_of(dim);
+  const int64_t chunks = rows * ld / 8;
+  hipLaunchKernelGGL(xent_lay_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, from, rows, dim, ld,
+                     static_cast<unsigned short*>(room));
+  return {room, rows, ld, rows * ld};
 }
 
-// dW of a piece.  Rows left out count for nothing, whatever their features hold.
-template <typename T>
-__global__ __launch_bounds__(256) void xent_dw_kernel(XentArgs a, const float* dz, int64_t v0, int64_t count) {
-  const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  const T* h = static_cast<const T*>(a.h);
-  tile_product([&](int64_t m, int64_t k) { return m < count ? dz[k * count + m] : 0.0f; },
-               [&](int64_t k, int64_t n) { return n < a.dim && a.labels[k] != a.ignore ? widen(h[k * a.dim + n]) : 0.0f; },
-               m0, n0, a.rows, acc);
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t v = m0 + ty * 4 + i, k = n0 + tx * 4 + j;
-      if (v < count && k < a.dim) static_cast<T*>(a.dw)[(v0 + v) * a.dim + k] = narrow<T>(acc[i][j]);
-    }
-}
-
-static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
-static int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
-static int64_t piece_of(int64_t rows, int64_t classes) {
-  return std::min<int64_t>(classes, std::max<int64_t>(kTile, kPieceBytes / 4 / rows / kTile * kTile));
-}
-
-size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int, bool backward) {
-  if (backward) return align256(rows * piece_of(rows, classes) * 4) + align256(rows * dim * 4);
-  return align256(rows * tiles_of(classes) * sizeof(float2)) + 2 * align256(rows * 4);
-}
-
-template <typename T>
-static hipError_t xent_fwd(const XentArgs& a, hipStream_t st) {
-  const int64_t tiles = tiles_of(a.classes);
-  char* ws = static_cast<char*>(a.ws);
-  float2* part = reinterpret_cast<float2*>(ws);
-  float* picked = reinterpret_cast<float*>(ws + align256(a.rows * tiles * sizeof(float2)));
-  float* each = a.reduction == kEach ? a.loss : picked + align256(a.rows * 4) / 4;
-  hipLaunchKernelGGL(xent_sums_kernel<T>, dim3((unsigned)tiles, (unsigned)tiles_of(a.rows)), dim3(256), 0, st, a, part,
-                     picked, tiles);
-  hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)a.rows), dim3(64), 0, st, a, part, picked, each, tiles);
-  hipLaunchKernelGGL(xent_mean_kernel, dim3(1), dim3(256), 0, st, a, each);
+// T: element type of the arguments, E: of the products' operands
+template <typename T, typename E>
+static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
+  const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
+  Room room{static_cast<char*>(a.ws)};
+  void *lay_h = room.take(p.lay_h), *lay_w = room.take(p.lay_w_fwd);
+  float2* part = static_cast<float2*>(room.take(p.part));
+  float* picked = static_cast<float*>(room.take(p.picked));
+  float* each = static_cast<float*>(room.take(p.each));
+  RowSum* row_sums = static_cast<RowSum*>(room.take(p.row_sums));
+  if (a.reduction == kEach) each = a.loss;
+  const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
+  ProductArgs g{};
+  g.b = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), st);
+  g.N = a.rows;
+  g.K = a.dim;
+  g.planes = planes_of(dtype);
+  g.splits = 1;
+  g.labels = a.labels;
+  g.part = part;
+  g.parts = p.parts;
+  g.picked = picked;
+  const bool own = as_it_is(w, a.dim, dtype);
+  const ProductPlan& plan = kPlans[p.fwd_shape];
+  // (all classes at once where nothing is laid out, but no more blocks than a grid may have)
+  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 22) / ((a.rows + plan.bn - 1) / plan.bn)) * plan.bm;
+  const int64_t piece = std::min(own ? a.classes : p.fwd_piece, std::max<int64_t>(256, most / 256 * 256));
+  hipError_t e = hipSuccess;
+  for (int64_t v0 = 0; v0 < a.classes && e == hipSuccess; v0 += piece) {
+    const int64_t count = std::min(piece, a.classes - v0);
+    g.a = laid(w + v0 * a.dim, count, a.dim, lay_w, own, st);
+    g.M = count;
+    g.v0 = v0;
+    g.part0 = v0 / plan.bm * plan.wm;
+    e = launch_product<E, T>(kLogits, true, p.fwd_shape, g, st);
+  }
+  if (e != hipSuccess) return e;
+  int team = 64;
+  while (team > 1 && team / 2 >= p.parts) team /= 2;
+  hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, part, picked, each,
+                     p.parts, team);
+  if (a.reduction != kEach || a.counted) {
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(256, a.rows / 8192));
+    const int64_t per = (a.rows + blocks - 1) / blocks;
+    hipLaunchKernelGGL(xent_sum_kernel, dim3((unsigned)blocks), dim3(kSumThreads), 0, st, a, each, per, row_sums);
+    if (blocks > 1) hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(64), 0, st, a, row_sums, (int)blocks);
+  }
   return hipGetLastError();
 }
 
 template <typename T>
-static hipError_t xent_bwd(const XentArgs& a, hipStream_t st) {
-  const int64_t piece = piece_of(a.rows, a.classes);
-  char* ws = static_cast<char*>(a.ws);
-  float* dz = reinterpret_cast<float*>(ws);
-  float* sum = reinterpret_cast<float*>(ws + align256(a.rows * piece * 4));
-  for (int64_t v0 = 0; v0 < a.classes; v0 += piece) {
-    const int64_t count = std::min(piece, a.classes - v0);
-    const unsigned rt = (unsigned)tiles_of(a.rows), vt = (unsigned)tiles_of(count), dt = (unsigned)tiles_of(a.dim);
-    hipLaunchKernelGGL(xent_dz_kernel<T>, dim3(vt, rt), dim3(256), 0, st, a, dz, v0, count);
-    if (a.dh) hipLaunchKernelGGL(xent_dh_kernel<T>, dim3(dt, rt), dim3(256), 0, st, a, dz, sum, v0, count);
-    if (a.dw) hipLaunchKernelGGL(xent_dw_kernel<T>, dim3(dt, vt), dim3(256), 0, st, a, dz, v0, count);
+static void xent_out(const float* sums, int splits, int64_t n, const float* scale, T* out, hipStream_t st) {
+  const unsigned blocks = (unsigned)std::min<int64_t>((n + 255) / 256, 4096);
+  hipLaunchKernelGGL(xent_out_kernel<T>, dim3(blocks), dim3(256), 0, st, sums, splits, n, scale, out);
+}
+
+template <typename T, typename E>
+static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
+  const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
+  Room room{static_cast<char*>(a.ws)};
+  void *lay_h = room.take(p.lay_h), *lay_w = room.take(p.lay_w), *dz = room.take(p.dz);
+  float *sums_h = static_cast<float*>(room.take(p.sums_h)), *sums_w = static_cast<float*>(room.take(p.sums_w));
+  float* row_scale = static_cast<float*>(room.take(p.row_scale));
+  unsigned long long* keep = static_cast<unsigned long long*>(room.take(p.keep));
+  float* scale = static_cast<float*>(room.take(p.scalars));
+  const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
+  const int P = planes_of(dtype);
+  const bool half = dtype == kF16;
+  if (half && a.reduction == kEach)
+    hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a.up, a.rows, scale + 1);
+  hipLaunchKernelGGL(xent_scale_kernel, dim3((unsigned)((a.rows + 255) / 256)), dim3(256), 0, st, a, half, scale + 1, row_scale,
+                     keep, scale);
+  const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), st);
+  const bool own = as_it_is(w, a.dim, dtype);
+  hipError_t e = hipSuccess;
+  for (int64_t v0 = 0; v0 < a.classes; v0 += p.piece) {
+    const int64_t count = std::min(p.piece, a.classes - v0), ld = up_to(count, 8);
+    const Matrix wm = laid(w + v0 * a.dim, count, a.dim, lay_w, own, st);
+    const Matrix zm{dz, a.rows, ld, a.rows * ld};
+    ProductArgs g{};
+    g.planes = P;
+    g.scale = scale;
+    // dz of the piece
+    g.a = wm; g.b = hm; g.M = count; g.N = a.rows; g.K = a.dim; g.splits = 1;
+    g.labels = a.labels; g.ignore = a.ignore; g.v0 = v0; g.lse = a.lse; g.row_scale = row_scale;
+    g.dz = dz; g.dz_ld = ld; g.dz_plane = a.rows * ld;
+    if ((e = launch_product<E, T>(kLogits, false, p.shape, g, st)) != hipSuccess) return e;
+    if (a.dh) {
+      g.a = wm; g.b = zm; g.M = a.dim; g.N = a.rows; g.K = count;
+      g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape));
+      g.sums = p.hidden_sums ? sums_h : nullptr;
+      g.add = v0 > 0;
+      g.out = a.dh;
+      if ((e = launch_product<E, T>(kHidden, false, p.hidden_shape, g, st)) != hipSuccess) return e;
+    }
+    if (a.dw) {
+      T* out = static_cast<T*>(a.dw) + v0 * a.dim;
+      g.a = hm; g.b = zm; g.M = a.dim; g.N = count; g.K = a.rows; g.keep = keep;
+      g.splits = p.weight_splits;
+      g.sums = p.weight_splits > 1 ? sums_w : nullptr;
+      g.add = 0;
+      g.out = out;
+      if ((e = launch_product<E, T>(kWeight, false, p.weight_shape, g, st)) != hipSuccess) return e;
+      if (g.sums) xent_out(sums_w, p.weight_splits, count * a.dim, scale, out, st);
+    }
   }
+  if (a.dh && p.hidden_sums) xent_out(sums_h, p.hidden_splits, a.rows * a.dim, scale, static_cast<T*>(a.dh), st);
   return hipGetLastError();
 }
 
 hipError_t launch_xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
-  return dtype == kF32 ? xent_fwd<float>(a, st) : dtype == kF16 ? xent_fwd<half_t>(a, st) : xent_fwd<bf16_t>(a, st);
+  return dtype == kF32   ? xent_fwd<float, bf16_t>(a, dtype, st)
+         : dtype == kF16 ? xent_fwd<half_t, half_t>(a, dtype, st)
+                         : xent_fwd<bf16_t, bf16_t>(a, dtype, st);
 }
 hipError_t launch_xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
-  return dtype == kF32 ? xent_bwd<float>(a, st) : dtype == kF16 ? xent_bwd<half_t>(a, st) : xent_bwd<bf16_t>(a, st);
+  return dtype == kF32   ? xent_bwd<float, bf16_t>(a, dtype, st)
+         : dtype == kF16 ? xent_bwd<half_t, half_t>(a, dtype, st)
+                         : xent_bwd<bf16_t, bf16_t>(a, dtype, st);
 }
 
 }  // namespace ecc

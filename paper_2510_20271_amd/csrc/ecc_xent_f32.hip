@@ -1,0 +1,6 @@
+// Products of the linear head's cross entropy for float32 (planes of bfloat16).
+#include "ecc_xent_launch.h"
+
+namespace ecc {
+template hipError_t launch_product<bf16_t, float>(int, bool, int, ProductArgs, hipStream_t);
+}

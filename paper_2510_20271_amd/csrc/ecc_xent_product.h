@@ -1,0 +1,355 @@
+// The matrix products of the linear head's cross entropy on the matrix cores, for 16-bit elements summed in float32:
+//   kLogits  C[v][i] = sum_k W[v][k] H[i][k]    logits of a tile, consumed where they are made: a maximum and a sum for each
+//                                               row (forward), or their gradient dz (backward)
+//   kHidden  C[k][i] = sum_v W[v][k] dZ[i][v]   gradient of hidden
+//   kWeight  C[k][v] = sum_i H[i][k] dZ[i][v]   gradient of the weight
+// The product is transposed against its result's layout: the accumulators of a 32 x 32 matrix instruction hold, in lane l,
+// column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4, so a lane has a row's logits side by side (their maximum and sum need
+// no exchange but one between two lanes) and four neighbours along a result's row (stores of 8 or 16 bytes).
+//
+// float32 operands are three bfloat16 planes, x = x1 + x2 + x3, each the leading 8 bits of what is left: exact.  A product is
+// then six products of planes, x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1; what is left out is below 2^-23 of |x| |y|.  Six
+// bfloat16 instructions stand against sixteen times the float32 instruction's rate.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ecc_types.h"
+
+namespace ecc {
+
+constexpr int kLogits = 0, kHidden = 1, kWeight = 2;
+constexpr int kDepth = 64;  // of a tile along the summed axis
+
+// A matrix of 16-bit elements [planes][rows][ld], ld a multiple of 8, 16-byte aligned; elements between a row's end and ld are 0.
+struct Matrix {
+  const void* p;
+  int64_t rows, ld, plane;  // plane: elements from one plane to the next
+};
+
+struct ProductArgs {
+  Matrix a, b;         // operands; summed along their rows' elements (kLogits: both; kHidden: b), else along their rows
+  int64_t M, N, K;     // of C; K: elements summed along (rows of the operand that is summed along its rows)
+  int planes;          // 1, or 3
+  int tiles_m, tiles_n;
+  int splits;          // the summed axis in so many runs of `steps` tiles, each with a result of its own
+  int steps;           // tiles of the summed axis of a run; all: total
+  int total;
+  const unsigned long long* keep;  // kWeight: bit i of the rows that count (others read as zeros)
+  // results
+  float* sums;         // kHidden, kWeight: [splits][N][M], or null: straight to out
+  int add;             //   added to what is there
+  void* out;           // [N][M], scaled by *scale
+  const float* scale;
+  // kLogits
+  const int64_t* labels;
+  int64_t v0;          // the first class of this piece (M: its classes)
+  float2* part;        // forward: [N][parts], parts part0 ..
+  int64_t parts, part0;
+  float* picked;       // forward: the label's logit
+  const float *lse, *row_scale;  // backward
+  void* dz;            // backward: [planes][N][dz_ld]
+  int64_t dz_ld, dz_plane;
+  int64_t ignore;
+};
+
+template <typename T> struct Lanes;
+template <> struct Lanes<bf16_t> {
+  using V8 = __bf16 __attribute__((ext_vector_type(8)));
+};
+template <> struct Lanes<half_t> {
+  using V8 = _Float16 __attribute__((ext_vector_type(8)));
+};
+using Acc = float __attribute__((ext_vector_type(16)));
+using Quad = short __attribute__((ext_vector_type(4)));
+using LdsVoid = __attribute__((address_space(3))) void;
+
+__device__ __forceinline__ Acc mma(Lanes<bf16_t>::V8 a, Lanes<bf16_t>::V8 b, Acc c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ Acc mma(Lanes<half_t>::V8 a, Lanes<half_t>::V8 b, Acc c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// x as three bfloat16 values that add up to it.  They have the sign of x, and where x is not 0 none is: an empty one is the
+// least normal number, so that an Inf meets no zero in the six products that its own product does not (Inf times x is an Inf
+// of the right sign; the error is 2^-126 and counts for nothing).  NaN: NaN and zeros.
+__device__ __forceinline__ void split3(float x, unsigned short (&p)[3]) {
+  const unsigned bits = __float_as_uint(x);
+  const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+  const float r1 = finite ? x - __uint_as_float(bits & 0xffff0000u) : 0.0f;
+  const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
+  p[0] = (unsigned short)(bits >> 16);
+  p[1] = (unsigned short)(__float_as_uint(r1) >> 16);
+  p[2] = (unsigned short)(__float_as_uint(r2) >> 16);
+  if (!finite && (bits & 0x007fffffu)) p[0] = 0x7fc0;
+  else if (p[0] & 0x7fff) {
+    const unsigned short least = (unsigned short)((p[0] & 0x8000) | 0x0080);
+    if (!(p[1] & 0x7fff)) p[1] = least;
+    if (!(p[2] & 0x7fff)) p[2] = least;
+  }
+}
+
+constexpr int kFar = 0x7fffff00;       // an offset that no buffer holds: such a lane's 16 bytes read as zeros
+constexpr int64_t kReach = 0x40000000;  // what a tile's offsets stay below
+
+// One operand's tile in LDS, SIDE x kDepth, and how a wave fetches and reads it.  Fetches go straight to LDS, 1 KB a wave
+// instruction, to consecutive 16-byte chunks; which chunk of its row a lane fetches is permuted so that reading is free of bank
+// conflicts.
+// ALONG: the operand's rows run along the summed axis: rows of 64 elements, chunk c of row r at place c ^ (r & 7).
+// Otherwise the tile has 64 rows of SIDE elements, and is read through the transposing LDS read: 16 lanes get 16 neighbouring
+// elements of 4 rows, transposed.  Four rows and their 64 bytes fill the banks once: chunk c of row r at c ^ 4 (r & 3) (for
+// rows of 128 bytes, of which two fill the banks, c ^ 4 (r / 2 & 1); rows of 64 bytes as they are).
+template <typename T, bool ALONG, int SIDE, int WAVES>
+struct Tile {
+  static constexpr int kBytes = SIDE * kDepth * 2;
+  static constexpr int kFetches = kBytes / 1024;
+  static constexpr int kEach = (kFetches + WAVES - 1) / WAVES;
+  static constexpr int kRow = ALONG ? 8 : SIDE / 8;  // chunks of a row
+  using V8 = typename Lanes<T>::V8;
+  int offset[kEach];  // of this lane's chunk, in bytes from the tile's origin
+  int mark[kEach];    // ALONG: the chunk's first element along the summed axis; otherwise its row
+
+  __device__ __forceinline__ static int place(int row, int c) {
+    if (ALONG) return c ^ (row & 7);
+    if (kRow >= 16) return c ^ ((row & 3) << 2);
+    if (kRow == 8) return c ^ ((row >> 1 & 1) << 2);
+    return c;
+  }
+  // origin: the tile's first row (ALONG) or column
+  __device__ __forceinline__ void init(const Matrix& m, int64_t origin, int wave, int lane) {
+#pragma unroll
+    for (int f = 0; f < kEach; ++f) {
+      const int at = (wave * kEach + f) * 64 + lane, row = at / kRow, c = place(row, at % kRow);
+      offset[f] = (int)(row * m.ld * 2) + c * 16;
+      mark[f] = ALONG ? c * 8 : row;
+      if (!ALONG && origin + c * 8 >= m.ld) offset[f] = kFar;
+    }
+  }
+  // tile `k` along the summed axis of plane `plane` to LDS at `to`; keep: the rows that count (not ALONG)
+  __device__ __forceinline__ void fetch(const Matrix& m, int64_t origin, int64_t K, int k, int plane, unsigned char* to, int wave,
+                                        unsigned long long keep) const {
+    const int64_t first = ALONG ? origin * m.ld : (int64_t)k * kDepth * m.ld + origin;
+    const int64_t left = ALONG ? (m.rows - origin) * m.ld : (K - (int64_t)k * kDepth) * m.ld - origin;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<unsigned short*>(static_cast<const unsigned short*>(m.p) + plane * m.plane + first), 0,
+        (int)(left * 2 < kReach ? left * 2 : kReach), 0x00020000);
+    const int end = (int)m.ld - k * kDepth;  // ALONG: elements of a row from here
+#pragma unroll
+    for (int f = 0; f < kEach; ++f) {
+      if (kFetches % WAVES == 0 || wave * kEach + f < kFetches) {
+        int at = offset[f];
+        if (ALONG) at = mark[f] < end ? at : kFar;
+        else at = (keep >> mark[f]) & 1 ? at : kFar;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)(to + (wave * kEach + f) * 1024), 16, at,
+                                                 ALONG ? __builtin_amdgcn_readfirstlane(k * kDepth * 2) : 0, 0, 0);
+      }
+    }
+  }
+  // operand of a matrix instruction: 32 rows / columns from `side`, 16 elements of the summed axis from 16 ks
+  __device__ __forceinline__ static V8 read(const unsigned char* from, int side, int ks, int lane) {
+    if (ALONG) {
+      const int row = side + (lane & 31);
+      return *reinterpret_cast<const V8*>(from + row * 128 + place(row, ks * 2 + (lane >> 5)) * 16);
+    }
+    const int q = lane >> 4, i = lane & 15, row = ks * 16 + (q >> 1) * 8 + (i >> 2), col = side + (q & 1) * 16 + (i & 3) * 4;
+    typedef __attribute__((address_space(3))) Quad LdsQuad;
+    // (rows + 4: the same place)
+    const unsigned char* at = from + row * (SIDE * 2) + place(row, col >> 3) * 16 + (i & 1) * 8;
+    union { Quad q[2]; V8 v; } u;
+    u.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad*)(at));
+    u.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad*)(at + 4 * SIDE * 2));
+    return u.v;
+  }
+};
+
+// Blocks in an order in which those that run at a time share operands: each of the eight dies takes a run of tiles, in bands of
+// four tiles of M, M fastest.
+__device__ __forceinline__ void tile_of(int block, int blocks, int tiles_m, int tiles_n, int& m, int& n, int& split) {
+  const int each = blocks / 8, over = blocks % 8, die = block % 8;
+  const int at = die * each + (die < over ? die : over) + block / 8;
+  const int tiles = tiles_m * tiles_n;
+  split = at / tiles;
+  const int t = at - split * tiles, band = t / (4 * tiles_n), in = t - band * 4 * tiles_n;
+  const int high = min(4, tiles_m - band * 4);
+  n = in / high;
+  m = band * 4 + in - n * high;
+}
+
+// a distance between classes as far as a tile is concerned
+__device__ __forceinline__ int near(int64_t d) { return (int)(d < -1 ? -1 : d > 1024 ? 1024 : d); }
+
+// O: element type of the result;  BM x BN: a block's tile of C, WM x WN waves
+template <typename T, typename O, int KIND, bool FORWARD, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs g) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+  using TA = Tile<T, KIND == kLogits, BM, kWaves>;
+  using TB = Tile<T, KIND != kWeight, BN, kWaves>;
+  constexpr int kBoth = TA::kBytes + TB::kBytes;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int tm, tn, split;
+  tile_of((int)blockIdx.x, (int)gridDim.x, g.tiles_m, g.tiles_n, tm, tn, split);
+  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int k0 = split * g.steps, ktiles = min(g.steps, g.total - k0), turns = ktiles * (g.planes == 1 ? 1 : 6);
+  TA ta;
+  TB tb;
+  ta.init(g.a, m0, wave, lane);
+  tb.init(g.b, n0, wave, lane);
+  Acc acc[TM][TN] = {};
+
+  int lk = k0, lj = 0;  // the next fetch: tile and pair of planes
+  const auto fetch = [&](int turn) {
+    // pairs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), two bits each
+    const int pa = g.planes == 1 ? 0 : (0x0850 >> (2 * lj)) & 3, pb = g.planes == 1 ? 0 : (0x0244 >> (2 * lj)) & 3;
+    unsigned char* to = smem + (turn & 1) * kBoth;
+    const unsigned long long keep = KIND == kWeight ? g.keep[lk] : ~0ull;
+    ta.fetch(g.a, m0, g.K, lk, pa, to, wave, keep);
+    tb.fetch(g.b, n0, g.K, lk, pb, to + TA::kBytes, wave, ~0ull);
+    if (g.planes == 1 || ++lj == 6) {
+      lj = 0;
+      ++lk;
+    }
+  };
+  const int am = (wave % WM) * (BM / WM), bn = (wave / WM) * (BN / WN);
+  fetch(0);
+  for (int t = 0; t < turns; ++t) {
+    __syncthreads();  // the tile is there, and the one before has been read
+    if (t + 1 < turns) fetch(t + 1);
+    const unsigned char* from = smem + (t & 1) * kBoth;
+#pragma unroll
+    for (int ks = 0; ks < kDepth / 16; ++ks) {
+      typename TA::V8 a[TM], b[TN];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) a[i] = TA::read(from, am + i * 32, ks, lane);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[j] = TB::read(from + TA::kBytes, bn + j * 32, ks, lane);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mma(a[i], b[j], acc[i][j]);
+    }
+  }
+
+  const int rows0 = 4 * (lane >> 5);  // accumulator r is row 8 (r / 4) + rows0 + r % 4 of its 32
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int64_t n = n0 + bn + j * 32 + (lane & 31);
+    const bool in = n < g.N;
+    if constexpr (KIND == kLogits && FORWARD) {
+      const int want = near(in ? g.labels[n] - g.v0 - m0 - am - rows0 : -1), left = near(g.M - m0 - am - rows0);
+      float top = -INFINITY, sum = 0.0f, picked = 0.0f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = i * 32 + 8 * (r / 4) + r % 4;
+          if (row < left) top = fmaxf(top, acc[i][j][r]);
+          picked = row == want ? acc[i][j][r] : picked;
+        }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = i * 32 + 8 * (r / 4) + r % 4;
+          if (row < left) sum += __expf(acc[i][j][r] - base);
+        }
+      sum += __shfl_xor(sum, 32);
+      if (want >= 0 && want < min(left, TM * 32) && !(want & 4)) g.picked[n] = picked;  // (a lane has rows 0 .. 3 of every 8)
+      if (in && lane < 32) g.part[n * g.parts + g.part0 + (int64_t)tm * WM + wave % WM] = make_float2(top, sum);
+    } else if constexpr (KIND == kLogits) {
+      const int64_t label = in ? g.labels[n] : -1;
+      const int want = near(label - g.v0 - m0 - am - rows0), left = near(g.M - m0 - am - rows0);
+      const bool counts = in && label != g.ignore;
+      const float lse = in ? g.lse[n] : 0.0f, scale = in ? g.row_scale[n] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t v = m0 + am + i * 32 + 8 * q + rows0;  // four classes from here
+          float f[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int row = i * 32 + 8 * q + r;
+            const float p = __expf(acc[i][j][q * 4 + r] - lse) - (row == want ? 1.0f : 0.0f);
+            f[r] = counts && row < left ? p * scale : 0.0f;
+          }
+          if (!in || v >= g.dz_ld) continue;  // (dz_ld is a multiple of 8)
+          unsigned short* to = static_cast<unsigned short*>(g.dz) + n * g.dz_ld + v;
+          if (g.planes == 1) {
+            T h[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) h[r] = narrow<T>(f[r]);
+            uint2 w;
+            __builtin_memcpy(&w, h, 8);
+            *reinterpret_cast<uint2*>(to) = w;
+          } else {
+            unsigned short s[4][3];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) split3(f[r], s[r]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+              const uint2 w = make_uint2((unsigned)s[0][k] | (unsigned)s[1][k] << 16, (unsigned)s[2][k] | (unsigned)s[3][k] << 16);
+              *reinterpret_cast<uint2*>(to + k * g.dz_plane) = w;
+            }
+          }
+        }
+    } else {
+      const float scale = g.sums ? 1.0f : *g.scale;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t m = m0 + am + i * 32 + 8 * q + rows0;
+          if (!in || m >= g.M) continue;
+          float f[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) f[r] = acc[i][j][q * 4 + r];
+          const bool four = g.M % 4 == 0;
+          if (g.sums) {
+            float* to = g.sums + ((int64_t)split * g.N + n) * g.M + m;
+            if (four) {
+              float4 w = make_float4(f[0], f[1], f[2], f[3]);
+              if (g.add) {
+                const float4 o = *reinterpret_cast<const float4*>(to);
+                w.x += o.x; w.y += o.y; w.z += o.z; w.w += o.w;
+              }
+              *reinterpret_cast<float4*>(to) = w;
+            } else {
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (m + r < g.M) to[r] = g.add ? to[r] + f[r] : f[r];
+            }
+          } else {
+            O* to = static_cast<O*>(g.out) + n * g.M + m;
+            O h[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) h[r] = narrow<O>(f[r] * scale);
+            if (four && (reinterpret_cast<uintptr_t>(g.out) & (sizeof(O) * 4 - 1)) == 0) {
+              struct alignas(sizeof(O) * 4) Four { O e[4]; } w;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) w.e[r] = h[r];
+              *reinterpret_cast<Four*>(to) = w;
+            } else {
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (m + r < g.M) to[r] = h[r];
+            }
+          }
+        }
+    }
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------
+// Which tile: 0: 256 x 256 (8 waves), 1: 128 x 128 (4 waves, two blocks a CU), 2: 128 x 32, 3: 32 x 128
+struct ProductPlan { int shape, bm, bn, wm; };
+constexpr ProductPlan kPlans[] = {{0, 256, 256, 2}, {1, 128, 128, 2}, {2, 128, 32, 4}, {3, 32, 128, 1}};
+
+// g.a .. g.K, planes, splits set; tiles, steps and total are filled in here
+template <typename T, typename O>
+hipError_t launch_product(int kind, bool forward, int shape, ProductArgs g, hipStream_t st);
+
+}  // namespace ecc
