@@ -96,7 +96,8 @@ constexpr int64_t kReach = 0x40000000;  // what a tile's offsets stay below
 // One operand's tile in LDS, SIDE x kDepth, and how a wave fetches and reads it.  Fetches go straight to LDS, 1 KB a wave
 // instruction, to consecutive 16-byte chunks; which chunk of its row a lane fetches is permuted so that reading is free of bank
 // conflicts.
-// ALONG: the operand's rows run along the summed axis: rows of 64 elements, chunk c of row r at place c ^ (r & 7).
+// ALONG: the operand's rows run along the summed axis: rows of 64 elements, two of which fill the banks, chunk c of row r at
+// place c ^ (r / 2 & 7): 16 lanes read one chunk of 16 rows at a time.
 // Otherwise the tile has 64 rows of SIDE elements, and is read through the transposing LDS read: 16 lanes get 16 neighbouring
 // elements of 4 rows, transposed.  Four rows and their 64 bytes fill the banks once: chunk c of row r at c ^ 4 (r & 3) (for
 // rows of 128 bytes, of which two fill the banks, c ^ 4 (r / 2 & 1); rows of 64 bytes as they are).
@@ -106,12 +107,13 @@ struct Tile {
   static constexpr int kFetches = kBytes / 1024;
   static constexpr int kEach = (kFetches + WAVES - 1) / WAVES;
   static constexpr int kRow = ALONG ? 8 : SIDE / 8;  // chunks of a row
+  static constexpr int kReads = ALONG ? 1 : 2;       // LDS instructions of an operand
   using V8 = typename Lanes<T>::V8;
   int offset[kEach];  // of this lane's chunk, in bytes from the tile's origin
   int mark[kEach];    // ALONG: the chunk's first element along the summed axis; otherwise its row
 
   __device__ __forceinline__ static int place(int row, int c) {
-    if (ALONG) return c ^ (row & 7);
+    if (ALONG) return c ^ (row >> 1 & 7);
     if (kRow >= 16) return c ^ ((row & 3) << 2);
     if (kRow == 8) return c ^ ((row >> 1 & 1) << 2);
     return c;
@@ -163,6 +165,17 @@ struct Tile {
   }
 };
 
+// The scheduler's order for a step: LDS reads of the next step's operands between this step's matrix instructions.
+template <int MMAS, int READS>
+__device__ __forceinline__ void interleave() {
+  constexpr int each = (READS + MMAS - 1) / MMAS;
+#pragma unroll
+  for (int i = 0; i < MMAS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, each, 0);
+  }
+}
+
 // Blocks in an order in which those that run at a time share operands: each of the eight dies takes a run of tiles, in bands of
 // four tiles of M, M fastest.
 __device__ __forceinline__ void tile_of(int block, int blocks, int tiles_m, int tiles_n, int& m, int& n, int& split) {
@@ -198,36 +211,42 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   tb.init(g.b, n0, wave, lane);
   Acc acc[TM][TN] = {};
 
-  int lk = k0, lj = 0;  // the next fetch: tile and pair of planes
+  int lk = k0, lj = 0;  // the next fetch: tile and pair of planes; its rows that count, read a turn ahead
+  unsigned long long keep = KIND == kWeight ? g.keep[lk] : ~0ull;
   const auto fetch = [&](int turn) {
     // pairs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), two bits each
     const int pa = g.planes == 1 ? 0 : (0x0850 >> (2 * lj)) & 3, pb = g.planes == 1 ? 0 : (0x0244 >> (2 * lj)) & 3;
     unsigned char* to = smem + (turn & 1) * kBoth;
-    const unsigned long long keep = KIND == kWeight ? g.keep[lk] : ~0ull;
     ta.fetch(g.a, m0, g.K, lk, pa, to, wave, keep);
     tb.fetch(g.b, n0, g.K, lk, pb, to + TA::kBytes, wave, ~0ull);
     if (g.planes == 1 || ++lj == 6) {
       lj = 0;
       ++lk;
+      if (KIND == kWeight) keep = g.keep[min(lk, g.total - 1)];
     }
   };
   const int am = (wave % WM) * (BM / WM), bn = (wave / WM) * (BN / WN);
   fetch(0);
   for (int t = 0; t < turns; ++t) {
     __syncthreads();  // the tile is there, and the one before has been read
-    if (t + 1 < turns) fetch(t + 1);
     const unsigned char* from = smem + (t & 1) * kBoth;
+    typename TA::V8 a[2][TM], b[2][TN];
+    const auto read = [&](int ks) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[ks & 1][j] = TB::read(from + TA::kBytes, bn + j * 32, ks, lane);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) a[ks & 1][i] = TA::read(from, am + i * 32, ks, lane);
+    };
+    read(0);
+    if (t + 1 < turns) fetch(t + 1);
 #pragma unroll
     for (int ks = 0; ks < kDepth / 16; ++ks) {
-      typename TA::V8 a[TM], b[TN];
-#pragma unroll
-      for (int i = 0; i < TM; ++i) a[i] = TA::read(from, am + i * 32, ks, lane);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) b[j] = TB::read(from + TA::kBytes, bn + j * 32, ks, lane);
+      if (ks + 1 < kDepth / 16) read(ks + 1);
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mma(a[i], b[j], acc[i][j]);
+        for (int j = 0; j < TN; ++j) acc[i][j] = mma(a[ks & 1][i], b[ks & 1][j], acc[i][j]);
+      interleave<TM * TN, TA::kReads * TM + TB::kReads * TN>();
     }
   }
 
