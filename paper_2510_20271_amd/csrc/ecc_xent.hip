@@ -157,14 +157,30 @@ __global__ __launch_bounds__(256) void xent_scale_kernel(XentArgs a, bool half, 
   if (i == 0) scale[0] = back;
 }
 
-// out = narrow(scale * sum of the splits)
+// out = narrow(scale * sum of the splits), `team` threads to an element, added in a fixed order
 template <typename O>
-__global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int splits, int64_t n, const float* scale, O* out) {
+__global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int splits, int64_t n, const float* scale, int team,
+                                                       O* out) {
+  __shared__ float room[256];
+  const int cols = 256 / team, col = threadIdx.x % cols, lane = threadIdx.x / cols;
   const float by = *scale;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    float s = sums[i];
-    for (int k = 1; k < splits; ++k) s += sums[k * n + i];
-    out[i] = narrow<O>(s * by);
+  for (int64_t i0 = (int64_t)blockIdx.x * cols; i0 < n; i0 += (int64_t)gridDim.x * cols) {  // (block-uniform)
+    const int64_t i = i0 + col;
+    float s = 0.0f;
+    if (i < n) {
+#pragma unroll 8
+      for (int k = lane; k < splits; k += team) s += sums[k * n + i];
+    }
+    if (team > 1) {
+      __syncthreads();
+      room[threadIdx.x] = s;
+      __syncthreads();
+      for (int o = team / 2; o > 0; o >>= 1) {
+        if (lane < o) room[threadIdx.x] = s = s + room[threadIdx.x + o * cols];
+        __syncthreads();
+      }
+    }
+    if (i < n && lane == 0) out[i] = narrow<O>(s * by);
   }
 }
 
@@ -180,16 +196,17 @@ static int ld_of(int dim) { return (int)up_to(dim, 8); }
 static int shape_of(int64_t M, int64_t N, int64_t runs) {
   if (N <= 32) return 2;
   if (M <= 32) return 3;
+  if (M <= 64 && N > 128) return 4;
   const int64_t large = (M + 255) / 256 * ((N + 255) / 256);
   return M > 128 && N > 128 && large * runs >= 256 ? 0 : 1;
 }
-// The summed axis in runs, so that blocks fill the card: eight tiles a run or more, results within kSumsBytes.
-static int splits_of(int64_t M, int64_t N, int64_t K, int shape) {
+// The summed axis in runs, so that blocks fill the card: eight turns a run or more, results within kSumsBytes.
+static int splits_of(int64_t M, int64_t N, int64_t K, int shape, int pairs) {
   const ProductPlan& p = kPlans[shape];
   const int64_t blocks = (M + p.bm - 1) / p.bm * ((N + p.bn - 1) / p.bn), total = (K + kDepth - 1) / kDepth;
-  const int64_t fill = shape == 0 ? 256 : shape == 1 ? 512 : 1024;
-  int64_t want = std::min(std::max<int64_t>(1, fill / blocks), std::max<int64_t>(1, total / 8));
-  want = std::max<int64_t>(1, std::min(want, kSumsBytes / (M * N * 4)));
+  const int64_t fill = shape == 0 ? 256 : 512;  // blocks that the card holds
+  int64_t want = std::min(std::max<int64_t>(1, fill / blocks), std::max<int64_t>(1, total * pairs / 8));
+  want = std::max<int64_t>(1, std::min({want, total, kSumsBytes / (M * N * 4)}));
   const int64_t steps = (total + want - 1) / want;
   return (int)((total + steps - 1) / steps);
 }
@@ -221,10 +238,10 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   p.shape = shape_of(p.piece, rows, 1);
   const int64_t long_k = std::max<int64_t>(1, p.piece / kDepth / 16), long_n = std::max<int64_t>(1, rows / kDepth / 16);
   p.hidden_shape = shape_of(dim, rows, long_k);
-  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape);
+  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape, P == 1 ? 1 : 6);
   p.hidden_sums = p.hidden_splits > 1 || p.piece < classes;
   p.weight_shape = shape_of(dim, p.piece, long_n);
-  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape);
+  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, P == 1 ? 1 : 6);
   p.lay_h = align256((size_t)rows * ld * 2 * P);
   p.lay_w = align256((size_t)p.piece * ld * 2 * P);
   p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * 2 * P);
@@ -284,7 +301,6 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   g.b = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), st);
   g.N = a.rows;
   g.K = a.dim;
-  g.planes = planes_of(dtype);
   g.splits = 1;
   g.labels = a.labels;
   g.part = part;
@@ -320,8 +336,9 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
 
 template <typename T>
 static void xent_out(const float* sums, int splits, int64_t n, const float* scale, T* out, hipStream_t st) {
-  const unsigned blocks = (unsigned)std::min<int64_t>((n + 255) / 256, 4096);
-  hipLaunchKernelGGL(xent_out_kernel<T>, dim3(blocks), dim3(256), 0, st, sums, splits, n, scale, out);
+  const int team = splits >= 64 ? 16 : splits >= 16 ? 4 : 1;
+  const unsigned blocks = (unsigned)std::min<int64_t>((n + 256 / team - 1) / (256 / team), 4096);
+  hipLaunchKernelGGL(xent_out_kernel<T>, dim3(blocks), dim3(256), 0, st, sums, splits, n, scale, team, out);
 }
 
 template <typename T, typename E>
@@ -334,7 +351,6 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   unsigned long long* keep = static_cast<unsigned long long*>(room.take(p.keep));
   float* scale = static_cast<float*>(room.take(p.scalars));
   const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
-  const int P = planes_of(dtype);
   const bool half = dtype == kF16;
   if (half && a.reduction == kEach)
     hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a.up, a.rows, scale + 1);
@@ -348,7 +364,6 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
     const Matrix wm = laid(w + v0 * a.dim, count, a.dim, lay_w, own, st);
     const Matrix zm{dz, a.rows, ld, a.rows * ld};
     ProductArgs g{};
-    g.planes = P;
     g.scale = scale;
     // dz of the piece
     g.a = wm; g.b = hm; g.M = count; g.N = a.rows; g.K = a.dim; g.splits = 1;
@@ -357,7 +372,7 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
     if ((e = launch_product<E, T>(kLogits, false, p.shape, g, st)) != hipSuccess) return e;
     if (a.dh) {
       g.a = wm; g.b = zm; g.M = a.dim; g.N = a.rows; g.K = count;
-      g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape));
+      g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape, planes_of(dtype) == 1 ? 1 : 6));
       g.sums = p.hidden_sums ? sums_h : nullptr;
       g.add = v0 > 0;
       g.out = a.dh;

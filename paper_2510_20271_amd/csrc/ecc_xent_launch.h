@@ -4,9 +4,9 @@
 
 namespace ecc {
 
-template <typename T, typename O, int BM, int BN, int WM, int WN>
+template <typename T, typename O, int BM, int BN, int WM, int WN, int STAGES>
 static hipError_t product_shape(int kind, bool forward, const ProductArgs& g, hipStream_t st) {
-  constexpr int kShared = 2 * (BM + BN) * kDepth * 2;
+  constexpr int kShared = STAGES * (BM + BN) * kDepth * 2;
   const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * g.splits)), block(WM * WN * 64);
   const auto go = [&](auto kernel) -> hipError_t {
     if (kShared > 64 << 10) {
@@ -16,10 +16,10 @@ static hipError_t product_shape(int kind, bool forward, const ProductArgs& g, hi
     hipLaunchKernelGGL(kernel, grid, block, kShared, st, g);
     return hipGetLastError();
   };
-  if (kind == kLogits) return forward ? go(product_kernel<T, O, kLogits, true, BM, BN, WM, WN>)
-                                      : go(product_kernel<T, O, kLogits, false, BM, BN, WM, WN>);
-  if (kind == kHidden) return go(product_kernel<T, O, kHidden, false, BM, BN, WM, WN>);
-  return go(product_kernel<T, O, kWeight, false, BM, BN, WM, WN>);
+  if (kind == kLogits) return forward ? go(product_kernel<T, O, kLogits, true, BM, BN, WM, WN, STAGES>)
+                                      : go(product_kernel<T, O, kLogits, false, BM, BN, WM, WN, STAGES>);
+  if (kind == kHidden) return go(product_kernel<T, O, kHidden, false, BM, BN, WM, WN, STAGES>);
+  return go(product_kernel<T, O, kWeight, false, BM, BN, WM, WN, STAGES>);
 }
 
 template <typename T, typename O>
@@ -31,10 +31,11 @@ hipError_t launch_product(int kind, bool forward, int shape, ProductArgs g, hipS
   g.steps = (g.total + g.splits - 1) / g.splits;
   g.splits = (g.total + g.steps - 1) / g.steps;  // (no run is empty)
   switch (shape) {
-    case 0: return product_shape<T, O, 256, 256, 2, 4>(kind, forward, g, st);
-    case 1: return product_shape<T, O, 128, 128, 2, 2>(kind, forward, g, st);
-    case 2: return product_shape<T, O, 128, 32, 4, 1>(kind, forward, g, st);
-    default: return product_shape<T, O, 32, 128, 1, 4>(kind, forward, g, st);
+    case 0: return product_shape<T, O, 256, 256, 2, 4, 2>(kind, forward, g, st);
+    case 1: return product_shape<T, O, 128, 128, 2, 2, 2>(kind, forward, g, st);
+    case 2: return product_shape<T, O, 128, 32, 4, 1, 4>(kind, forward, g, st);
+    case 3: return product_shape<T, O, 32, 128, 1, 4, 4>(kind, forward, g, st);
+    default: return product_shape<T, O, 64, 256, 1, 4, 2>(kind, forward, g, st);
   }
 }
 

@@ -30,7 +30,6 @@ struct Matrix {
 struct ProductArgs {
   Matrix a, b;         // operands; summed along their rows' elements (kLogits: both; kHidden: b), else along their rows
   int64_t M, N, K;     // of C; K: elements summed along (rows of the operand that is summed along its rows)
-  int planes;          // 1, or 3
   int tiles_m, tiles_n;
   int splits;          // the summed axis in so many runs of `steps` tiles, each with a result of its own
   int steps;           // tiles of the summed axis of a run; all: total
@@ -101,11 +100,33 @@ constexpr int64_t kReach = 0x40000000;  // what a tile's offsets stay below
 // Otherwise the tile has 64 rows of SIDE elements, and is read through the transposing LDS read: 16 lanes get 16 neighbouring
 // elements of 4 rows, transposed.  Four rows and their 64 bytes fill the banks once: chunk c of row r at c ^ 4 (r & 3) (for
 // rows of 128 bytes, of which two fill the banks, c ^ 4 (r / 2 & 1); rows of 64 bytes as they are).
+// where an operand's next tile is, uniform over the block
+template <bool ALONG>
+struct Cursor {
+  const char* at;
+  int64_t left;  // bytes of the operand from there
+  int64_t step;  // bytes to the next tile
+  int64_t plane;
+  __device__ __forceinline__ Cursor(const Matrix& m, int64_t origin, int64_t K, int k0) {
+    const int64_t first = ALONG ? origin * m.ld : (int64_t)k0 * kDepth * m.ld + origin;
+    at = static_cast<const char*>(m.p) + first * 2;
+    left = ((ALONG ? m.rows : K) * m.ld - first) * 2;
+    step = ALONG ? 0 : (int64_t)kDepth * m.ld * 2;
+    plane = m.plane * 2;
+  }
+  __device__ __forceinline__ int reach() const { return (int)(left < 0 ? 0 : left < kReach ? left : kReach); }
+  __device__ __forceinline__ void next() {
+    at += step;
+    left -= step;
+  }
+};
+
 template <typename T, bool ALONG, int SIDE, int WAVES>
 struct Tile {
   static constexpr int kBytes = SIDE * kDepth * 2;
   static constexpr int kFetches = kBytes / 1024;
-  static constexpr int kEach = (kFetches + WAVES - 1) / WAVES;
+  static constexpr int kEach = kFetches / WAVES;
+  static_assert(kFetches % WAVES == 0, "every wave fetches alike");
   static constexpr int kRow = ALONG ? 8 : SIDE / 8;  // chunks of a row
   static constexpr int kReads = ALONG ? 1 : 2;       // LDS instructions of an operand
   using V8 = typename Lanes<T>::V8;
@@ -128,24 +149,19 @@ struct Tile {
       if (!ALONG && origin + c * 8 >= m.ld) offset[f] = kFar;
     }
   }
-  // tile `k` along the summed axis of plane `plane` to LDS at `to`; keep: the rows that count (not ALONG)
-  __device__ __forceinline__ void fetch(const Matrix& m, int64_t origin, int64_t K, int k, int plane, unsigned char* to, int wave,
+  // A tile to LDS at `to`: the tile's origin is at `from`, which `left` bytes of the operand follow; k: its first element along
+  // the summed axis (ALONG: `from` is the row's first element); keep: the rows that count (not ALONG)
+  __device__ __forceinline__ void fetch(const char* from, int left, int ld, int k, unsigned char* to, int wave,
                                         unsigned long long keep) const {
-    const int64_t first = ALONG ? origin * m.ld : (int64_t)k * kDepth * m.ld + origin;
-    const int64_t left = ALONG ? (m.rows - origin) * m.ld : (K - (int64_t)k * kDepth) * m.ld - origin;
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<unsigned short*>(static_cast<const unsigned short*>(m.p) + plane * m.plane + first), 0,
-        (int)(left * 2 < kReach ? left * 2 : kReach), 0x00020000);
-    const int end = (int)m.ld - k * kDepth;  // ALONG: elements of a row from here
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, left, 0x00020000);
+    const int end = ld - k;  // ALONG: elements of a row from here
 #pragma unroll
     for (int f = 0; f < kEach; ++f) {
-      if (kFetches % WAVES == 0 || wave * kEach + f < kFetches) {
-        int at = offset[f];
-        if (ALONG) at = mark[f] < end ? at : kFar;
-        else at = (keep >> mark[f]) & 1 ? at : kFar;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)(to + (wave * kEach + f) * 1024), 16, at,
-                                                 ALONG ? __builtin_amdgcn_readfirstlane(k * kDepth * 2) : 0, 0, 0);
-      }
+      int at = offset[f];
+      if (ALONG) at = mark[f] < end ? at : kFar;
+      else at = (keep >> mark[f]) & 1 ? at : kFar;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)(to + (wave * kEach + f) * 1024), 16, at,
+                                               ALONG ? __builtin_amdgcn_readfirstlane(k * 2) : 0, 0, 0);
     }
   }
   // operand of a matrix instruction: 32 rows / columns from `side`, 16 elements of the summed axis from 16 ks
@@ -192,8 +208,15 @@ __device__ __forceinline__ void tile_of(int block, int blocks, int tiles_m, int 
 // a distance between classes as far as a tile is concerned
 __device__ __forceinline__ int near(int64_t d) { return (int)(d < -1 ? -1 : d > 1024 ? 1024 : d); }
 
-// O: element type of the result;  BM x BN: a block's tile of C, WM x WN waves
-template <typename T, typename O, int KIND, bool FORWARD, int BM, int BN, int WM, int WN>
+// Waits until all but the last N fetches of this wave have landed and its LDS reads are done, then for the other waves.
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// O: element type of the result;  BM x BN: a block's tile of C, WM x WN waves;  STAGES: tiles in LDS, all but one of them on
+// their way (thin tiles are computed faster than one arrives)
+template <typename T, typename O, int KIND, bool FORWARD, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs g) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
@@ -204,32 +227,41 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   int tm, tn, split;
   tile_of((int)blockIdx.x, (int)gridDim.x, g.tiles_m, g.tiles_n, tm, tn, split);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-  const int k0 = split * g.steps, ktiles = min(g.steps, g.total - k0), turns = ktiles * (g.planes == 1 ? 1 : 6);
+  constexpr int kPairs = sizeof(O) == 4 ? 6 : 1;  // products of planes
+  const int k0 = split * g.steps, ktiles = min(g.steps, g.total - k0), turns = ktiles * kPairs;
   TA ta;
   TB tb;
   ta.init(g.a, m0, wave, lane);
   tb.init(g.b, n0, wave, lane);
   Acc acc[TM][TN] = {};
 
-  int lk = k0, lj = 0;  // the next fetch: tile and pair of planes; its rows that count, read a turn ahead
-  unsigned long long keep = KIND == kWeight ? g.keep[lk] : ~0ull;
+  // the next fetch: tile, pair of planes, and the rows that count (read a turn ahead)
+  Cursor<KIND == kLogits> ca(g.a, m0, g.K, k0);
+  Cursor<KIND != kWeight> cb(g.b, n0, g.K, k0);
+  int lk = k0, lj = 0;
+  const auto* rows = (const __attribute__((address_space(4))) unsigned long long*)g.keep;  // (scalar reads)
+  unsigned long long keep = KIND == kWeight ? rows[lk] : ~0ull;
   const auto fetch = [&](int turn) {
     // pairs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), two bits each
-    const int pa = g.planes == 1 ? 0 : (0x0850 >> (2 * lj)) & 3, pb = g.planes == 1 ? 0 : (0x0244 >> (2 * lj)) & 3;
-    unsigned char* to = smem + (turn & 1) * kBoth;
-    ta.fetch(g.a, m0, g.K, lk, pa, to, wave, keep);
-    tb.fetch(g.b, n0, g.K, lk, pb, to + TA::kBytes, wave, ~0ull);
-    if (g.planes == 1 || ++lj == 6) {
+    const int64_t pa = kPairs == 1 ? 0 : (0x0850 >> (2 * lj) & 3) * ca.plane, pb = kPairs == 1 ? 0 : (0x0244 >> (2 * lj) & 3) * cb.plane;
+    unsigned char* to = smem + turn % STAGES * kBoth;
+    const bool any = turn < turns;  // (behind the last tile nothing is read: zeros go where no one looks)
+    ta.fetch(ca.at + pa, any ? ca.reach() : 0, (int)g.a.ld, lk * kDepth, to, wave, keep);
+    tb.fetch(cb.at + pb, any ? cb.reach() : 0, (int)g.b.ld, lk * kDepth, to + TA::kBytes, wave, ~0ull);
+    if (kPairs == 1 || ++lj == kPairs) {
       lj = 0;
       ++lk;
-      if (KIND == kWeight) keep = g.keep[min(lk, g.total - 1)];
+      ca.next();
+      cb.next();
+      if (KIND == kWeight) keep = rows[min(lk, g.total - 1)];
     }
   };
   const int am = (wave % WM) * (BM / WM), bn = (wave / WM) * (BN / WN);
-  fetch(0);
+#pragma unroll
+  for (int t = 0; t < STAGES - 1; ++t) fetch(t);
   for (int t = 0; t < turns; ++t) {
-    __syncthreads();  // the tile is there, and the one before has been read
-    const unsigned char* from = smem + (t & 1) * kBoth;
+    wait_and_meet<(STAGES - 2) * (TA::kEach + TB::kEach)>();  // the tile is there, and the one before has been read
+    const unsigned char* from = smem + t % STAGES * kBoth;
     typename TA::V8 a[2][TM], b[2][TN];
     const auto read = [&](int ks) {
 #pragma unroll
@@ -238,7 +270,6 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
       for (int i = 0; i < TM; ++i) a[ks & 1][i] = TA::read(from, am + i * 32, ks, lane);
     };
     read(0);
-    if (t + 1 < turns) fetch(t + 1);
 #pragma unroll
     for (int ks = 0; ks < kDepth / 16; ++ks) {
       if (ks + 1 < kDepth / 16) read(ks + 1);
@@ -247,8 +278,10 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mma(a[ks & 1][i], b[ks & 1][j], acc[i][j]);
       interleave<TM * TN, TA::kReads * TM + TB::kReads * TN>();
+      if (ks == 0) fetch(t + STAGES - 1);
     }
   }
+  wait_and_meet<0>();  // (the last fetches have to land before the block's LDS is another's)
 
   const int rows0 = 4 * (lane >> 5);  // accumulator r is row 8 (r / 4) + rows0 + r % 4 of its 32
 #pragma unroll
@@ -297,7 +330,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
           }
           if (!in || v >= g.dz_ld) continue;  // (dz_ld is a multiple of 8)
           unsigned short* to = static_cast<unsigned short*>(g.dz) + n * g.dz_ld + v;
-          if (g.planes == 1) {
+          if constexpr (kPairs == 1) {
             T h[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) h[r] = narrow<T>(f[r]);
@@ -363,11 +396,11 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------------
-// Which tile: 0: 256 x 256 (8 waves), 1: 128 x 128 (4 waves, two blocks a CU), 2: 128 x 32, 3: 32 x 128
-struct ProductPlan { int shape, bm, bn, wm; };
-constexpr ProductPlan kPlans[] = {{0, 256, 256, 2}, {1, 128, 128, 2}, {2, 128, 32, 4}, {3, 32, 128, 1}};
+// Tiles: 0: 256 x 256 (8 waves, a block a CU), 1: 128 x 128 (4 waves, two blocks), 2: 128 x 32, 3: 32 x 128, 4: 64 x 256
+struct ProductPlan { int bm, bn, wm; };
+constexpr ProductPlan kPlans[] = {{256, 256, 2}, {128, 128, 2}, {128, 32, 4}, {32, 128, 1}, {64, 256, 1}};
 
-// g.a .. g.K, planes, splits set; tiles, steps and total are filled in here
+// g.a .. g.K, splits set; tiles, steps and total are filled in here
 template <typename T, typename O>
 hipError_t launch_product(int kind, bool forward, int shape, ProductArgs g, hipStream_t st);
 
