@@ -5,6 +5,7 @@ current stream, every step of the computation runs inside libecc_hip.so.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 
@@ -370,6 +371,14 @@ def _on_current_device(t):
     """The stream is the current device's, so that is where the tensors have to be."""
     if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"tensors must be on the current device, got {t.device}")
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _on_device_of(t):
+    """A context in which the tensor's device is the current one."""
+    return _HERE if t.get_device() == torch._C._cuda_getDevice() else torch.cuda.device(t.device)
 
 
 def _room(need: int, device) -> torch.Tensor:

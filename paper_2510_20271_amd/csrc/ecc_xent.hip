@@ -47,6 +47,12 @@ __global__ __launch_bounds__(256) void xent_lay_kernel(const T* __restrict__ fro
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void xent_row(const XentArgs& a, int64_t row, float m, double s, const float* picked, float* each) {
+  const double lse = (double)m + log(s);
+  if (a.lse) a.lse[row] = (float)lse;
+  const int64_t label = a.labels[row];
+  each[row] = label == a.ignore ? 0.0f : label < 0 || label >= a.classes ? NAN : (float)(lse - (double)picked[row]);
+}
 // A row's tiles joined by `team` lanes (a power of two): lse, and the row's loss.
 __global__ __launch_bounds__(256) void xent_rows_kernel(XentArgs a, const float2* part, const float* picked, float* each,
                                                         int64_t parts, int team) {
@@ -60,11 +66,30 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(XentArgs a, const float2
   double s = 0.0;
   for (int64_t t = lane; t < parts; t += team) s += (double)p[t].y * (p[t].x == m ? 1.0 : (double)__expf(p[t].x - m));
   for (int o = team / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if (!in || lane != 0) return;
-  const double lse = (double)m + log(s);
-  if (a.lse) a.lse[row] = (float)lse;
-  const int64_t label = a.labels[row];
-  each[row] = label == a.ignore ? 0.0f : label < 0 || label >= a.classes ? NAN : (float)(lse - (double)picked[row]);
+  if (in && lane == 0) xent_row(a, row, m, s, picked, each);
+}
+// The same with a block for a row, where rows are few and tiles many (one row, 4096 tiles: 32 us by a wave, 6 by a block).
+__global__ __launch_bounds__(1024) void xent_long_row_kernel(XentArgs a, const float2* part, const float* picked, float* each,
+                                                             int64_t parts) {
+  __shared__ float top[16];
+  __shared__ double sum[16];
+  const int64_t row = blockIdx.x;
+  const float2* p = part + row * parts;
+  float m = -INFINITY;
+  for (int64_t t = threadIdx.x; t < parts; t += 1024) m = fmaxf(m, p[t].x);
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = m;
+  __syncthreads();
+  for (int k = 0; k < 16; ++k) m = fmaxf(m, top[k]);
+  double s = 0.0;
+  for (int64_t t = threadIdx.x; t < parts; t += 1024) s += (double)p[t].y * (p[t].x == m ? 1.0 : (double)__expf(p[t].x - m));
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if ((threadIdx.x & 63) == 0) sum[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  s = 0.0;
+  for (int k = 0; k < 16; ++k) s += sum[k];
+  xent_row(a, row, m, s, picked, each);
 }
 
 // Sum of the rows' losses and their count, a run of rows a block; one block: the loss itself.
@@ -321,10 +346,14 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
     e = launch_product<E, T>(kLogits, true, p.fwd_shape, g, st);
   }
   if (e != hipSuccess) return e;
-  int team = 64;
-  while (team > 1 && team / 2 >= p.parts) team /= 2;
-  hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, part, picked, each,
-                     p.parts, team);
+  if (a.rows < 512 && p.parts > 512) {
+    hipLaunchKernelGGL(xent_long_row_kernel, dim3((unsigned)a.rows), dim3(1024), 0, st, a, part, picked, each, p.parts);
+  } else {
+    int team = 64;
+    while (team > 1 && team / 2 >= p.parts) team /= 2;
+    hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, part, picked, each,
+                       p.parts, team);
+  }
   if (a.reduction != kEach || a.counted) {
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(256, a.rows / 8192));
     const int64_t per = (a.rows + blocks - 1) / blocks;

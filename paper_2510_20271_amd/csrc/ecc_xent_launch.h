@@ -30,11 +30,16 @@ hipError_t launch_product(int kind, bool forward, int shape, ProductArgs g, hipS
   g.total = (int)((g.K + kDepth - 1) / kDepth);
   g.steps = (g.total + g.splits - 1) / g.splits;
   g.splits = (g.total + g.steps - 1) / g.steps;  // (no run is empty)
+  const int turns = g.steps * (sizeof(O) == 4 ? 6 : 1);
   switch (shape) {
     case 0: return product_shape<T, O, 256, 256, 2, 4, 2>(kind, forward, g, st);
     case 1: return product_shape<T, O, 128, 128, 2, 2, 2>(kind, forward, g, st);
-    case 2: return product_shape<T, O, 128, 32, 4, 1, 4>(kind, forward, g, st);
-    case 3: return product_shape<T, O, 32, 128, 1, 4, 4>(kind, forward, g, st);
+    // four tiles in LDS leave room for half the blocks: only where there are tiles to come (one tile of 64 elements, 524288 x 64 x
+    // 21 in bfloat16: 20 us with two, 28 with four; six turns or more, 32 x 128 x 1000 in float32: 10.4 with two, 7.8 with four)
+    case 2: return turns < 4 ? product_shape<T, O, 128, 32, 4, 1, 2>(kind, forward, g, st)
+                             : product_shape<T, O, 128, 32, 4, 1, 4>(kind, forward, g, st);
+    case 3: return turns < 4 ? product_shape<T, O, 32, 128, 1, 4, 2>(kind, forward, g, st)
+                             : product_shape<T, O, 32, 128, 1, 4, 4>(kind, forward, g, st);
     default: return product_shape<T, O, 64, 256, 1, 4, 2>(kind, forward, g, st);
   }
 }

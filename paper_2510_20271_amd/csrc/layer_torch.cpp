@@ -8,40 +8,10 @@
 //
 // layer.py takes this path for plain contiguous float32 tensors outside function transforms and tracing; everything else
 // goes through its Python functions, whose results are the same.
-#include <torch/extension.h>
-
-#include <c10/hip/HIPStream.h>
-
-#include <string>
-
-#include "ecc.h"
+#include "layer_torch.h"
 
 namespace {
 
-using torch::Tensor;
-using torch::autograd::AutogradContext;
-using torch::autograd::variable_list;
-
-// What the library refuses is the Python binding's EccError, with its status, in the backward pass as well.
-void check(int status) {
-  if (status == ECC_OK) return;
-  const std::string message = ecc_last_error();  // (of this thread)
-  const py::gil_scoped_acquire gil;
-  const py::object type = py::module_::import("paper_2510_20271_amd.api").attr("EccError");
-  const py::object error = type(status, message);
-  PyErr_SetObject(type.ptr(), error.ptr());
-  throw py::error_already_set();
-}
-void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
-float* f32(const Tensor& t) { return t.defined() ? t.data_ptr<float>() : nullptr; }
-// Saved tensors come back from saved-tensor hooks, upstream gradients from anywhere: what the kernels are handed is as the
-// forward pass made it, or nothing (numel < 0: any number of elements).
-void check_device(const Tensor& t, at::ScalarType type, int64_t numel, const at::Device& device) {
-  TORCH_CHECK_VALUE(t.defined() && t.layout() == at::kStrided && t.has_storage() && t.is_contiguous() && t.device() == device,
-                    "tensors must be contiguous device tensors");
-  TORCH_CHECK_VALUE(t.scalar_type() == type && (numel < 0 || t.numel() == numel),
-                    "a saved tensor or gradient is not of the type or size that the forward pass left");
-}
 int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
 
 // One buffer of floats: the direction, then (where wanted) d chi / d tau and d chi / d u, each at a multiple of 256 bytes.
@@ -177,6 +147,7 @@ Tensor soft_angles(const Tensor& grid, const Tensor& theta, const Tensor& tau, d
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
+  bind_operators(m);
   // (without the interpreter's lock, as the Python function's library calls: a launch waits when the device's queue is full)
   m.def("soft_angles", &soft_angles, "Soft curves with the direction given by its angles, differentiable",
         py::call_guard<py::gil_scoped_release>());

@@ -14,6 +14,7 @@ Inputs must live on the GPU; there is no CPU path.
 """
 from __future__ import annotations
 
+import functools
 import math
 
 import torch
@@ -105,32 +106,67 @@ class _SoftECCAngles(torch.autograd.Function):
 _PLAIN = (torch.Tensor, torch.nn.Parameter)
 
 
-def _native_takes(grid, theta, tau, ndim: int) -> bool:
-    """What the C++ function is for: plain contiguous float32 tensors of the layer's shapes on one GPU, outside function
-    transforms, dispatch modes, tracing, compilation and forward-mode differentiation."""
-    return (type(grid) in _PLAIN and type(tau) in _PLAIN and grid.is_cuda and tau.is_cuda
-            and grid.dtype is torch.float32 and tau.dtype is torch.float32
-            and grid.dim() == ndim + 1 and tau.dim() == 1 and theta.dim() == 1
-            and grid.get_device() == tau.get_device() == theta.get_device()
-            and grid.is_contiguous() and tau.is_contiguous()
+def _plain(*tensors) -> bool:
+    """Tensors of no subclass (None passes), outside function transforms, dispatch modes, tracing, compilation and
+    forward-mode differentiation."""
+    return (all(t is None or type(t) in _PLAIN for t in tensors)
             and not torch._C._are_functorch_transforms_active() and torch._C._len_torch_dispatch_stack() == 0
             and torch._C._get_tracing_state() is None and not torch.compiler.is_compiling()
             and torch.autograd.forward_ad._current_level < 0)
 
 
-_soft_angles = None
+def _native_takes(grid, theta, tau, ndim: int) -> bool:
+    """What the C++ function is for: plain contiguous float32 tensors of the layer's shapes on one GPU, outside function
+    transforms, dispatch modes, tracing, compilation and forward-mode differentiation."""
+    return (_plain(grid, tau) and grid.is_cuda and tau.is_cuda
+            and grid.dtype is torch.float32 and tau.dtype is torch.float32
+            and grid.dim() == ndim + 1 and tau.dim() == 1 and theta.dim() == 1
+            and grid.get_device() == tau.get_device() == theta.get_device()
+            and grid.is_contiguous() and tau.is_contiguous())
 
 
-def _native():
-    global _soft_angles
-    if _soft_angles is None:
+class _Refuse(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, grad, *depends_on):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("this operator's backward pass is not differentiable a second time")
+
+
+def _once(backward):
+    """For a backward pass that is not differentiable itself: gradients made for a graph are tied to what they depend on,
+    the saved inputs included, by a function that refuses."""
+    @functools.wraps(backward)
+    def wrapped(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return out
+        depends_on = [t for t in (*grads, *ctx.saved_tensors) if t is not None and t.is_floating_point()]
+        return tuple(None if t is None else _Refuse.apply(t, *depends_on) for t in out)
+    return wrapped
+
+
+_native_module = None
+
+
+def _native_functions():
+    """The extension with the autograd functions in C++."""
+    global _native_module
+    if _native_module is None:
         api._lib.load()
         try:
             from . import _layer_native
         except ImportError as e:
             raise RuntimeError("_layer_native.so is missing: build it with `python -m paper_2510_20271_amd.build`") from e
-        _soft_angles = _layer_native.soft_angles
-    return _soft_angles
+        _native_module = _layer_native
+    return _native_module
+
+
+def _native():
+    return _native_functions().soft_angles
 
 
 def soft_ecc(grid, u, tau, alpha: float, lam: float, tilted_c: bool = False):

@@ -12,9 +12,9 @@ from __future__ import annotations
 import math
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import api
+from .layer import _native_functions, _once, _plain
 
 
 class LinearCrossEntropyFunction(torch.autograd.Function):
@@ -22,20 +22,19 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, hidden, weight, labels, ignore_index: int, reduction: str):
-        hidden, weight = hidden.detach(), weight.detach()
         keep = any(ctx.needs_input_grad[:2])
-        loss, lse, counted = api.ecc_xent_fwd(hidden, weight, labels, ignore_index, reduction, keep=keep)
+        loss, lse, counted = api.ecc_xent_fwd(hidden.detach(), weight.detach(), labels, ignore_index, reduction, keep=keep)
         ctx.ignore_index, ctx.reduction = ignore_index, reduction
         if keep:
             ctx.save_for_backward(hidden, weight, labels, lse, counted)
         return loss
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, grad_loss):
         hidden, weight, labels, lse, counted = ctx.saved_tensors
         skip = [n for n, need in zip(("grad_hidden", "grad_weight"), ctx.needs_input_grad) if not need]
-        with torch.cuda.device(hidden.device):
+        with api._on_device_of(hidden):
             grads = api.ecc_xent_bwd(hidden, weight, labels, grad_loss.contiguous(), lse, counted, ctx.ignore_index,
                                      ctx.reduction, skip=skip)
         return *grads, None, None, None
@@ -48,7 +47,10 @@ def linear_cross_entropy(hidden, weight, labels, ignore_index: int = -100, reduc
     makes its row's loss and gradients NaN."""
     if not hidden.is_cuda or not weight.is_cuda or not labels.is_cuda:
         raise ValueError("hidden, weight and labels must be on the GPU")
+    if not hidden.device == weight.device == labels.device:
+        raise ValueError(f"tensors must be on one device, got {hidden.device}, {weight.device} and {labels.device}")
     api._one_of(api._REDUCTIONS, reduction, "reduction")
+    api._one_of(api._OPERATOR_DTYPES, hidden.dtype, "the type of hidden")
     if hidden.dim() < 1 or weight.dim() != 2 or hidden.shape[-1] != weight.shape[1]:
         raise ValueError("hidden must be [..., dim] and weight [classes, dim]")
     if tuple(labels.shape) != tuple(hidden.shape[:-1]):
@@ -60,10 +62,13 @@ def linear_cross_entropy(hidden, weight, labels, ignore_index: int = -100, reduc
     if labels.numel() == 0:  # no row: no loss, gradients of zero
         nothing = (hidden.sum() * 0.0 + weight[:0].sum() * 0.0).float()
         return nothing if reduction != "none" else nothing + torch.zeros(labels.shape, device=hidden.device)
-    rows = hidden.reshape(-1, hidden.shape[-1]).contiguous()
-    with torch.cuda.device(hidden.device):
-        loss = LinearCrossEntropyFunction.apply(rows, weight.contiguous(), labels.reshape(-1).contiguous(),
-                                                int(ignore_index), reduction)
+    rows = (hidden if hidden.dim() == 2 else hidden.reshape(-1, hidden.shape[-1])).contiguous()
+    weight, flat = weight.contiguous(), labels.reshape(-1).contiguous()
+    with api._on_device_of(hidden):
+        if _plain(rows, weight, flat):
+            loss = _native_functions().linear_xent(rows, weight, flat, int(ignore_index), api._REDUCTIONS[reduction])
+        else:
+            loss = LinearCrossEntropyFunction.apply(rows, weight, flat, int(ignore_index), reduction)
     return loss.reshape(labels.shape) if reduction == "none" else loss
 
 

@@ -10,9 +10,9 @@ Inputs must live on the GPU; there is no CPU path.
 from __future__ import annotations
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import api
+from .layer import _native_functions, _once, _plain
 
 
 class GroupNormActFunction(torch.autograd.Function):
@@ -20,19 +20,18 @@ class GroupNormActFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, groups: int, eps: float, act: str):
-        x = x.detach()
-        y, stats = api.ecc_norm_fwd(x, groups, weight, bias, eps, act, keep=any(ctx.needs_input_grad[:3]))
+        y, stats = api.ecc_norm_fwd(x.detach(), groups, weight, bias, eps, act, keep=any(ctx.needs_input_grad[:3]))
         ctx.groups, ctx.act = groups, act
         if stats is not None:
             ctx.save_for_backward(x, weight, bias, stats)
         return y
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, grad_y):
         x, weight, bias, stats = ctx.saved_tensors
         skip = [n for n, need in zip(("grad_x", "grad_weight", "grad_bias"), ctx.needs_input_grad) if not need]
-        with torch.cuda.device(x.device):
+        with api._on_device_of(x):
             grads = api.ecc_norm_bwd(x, grad_y.contiguous(), ctx.groups, stats, weight, bias, ctx.act, skip=skip)
         return *grads, None, None, None
 
@@ -55,8 +54,16 @@ def group_norm_act(x, groups: int, weight=None, bias=None, eps: float = 1e-5, ac
         return x * 1.0 + sum(t.sum().to(x.dtype) * 0.0 for t in (weight, bias) if t is not None)
     weight = None if weight is None else weight.float().contiguous()
     bias = None if bias is None else bias.float().contiguous()
-    with torch.cuda.device(x.device):
-        return GroupNormActFunction.apply(x.contiguous(), weight, bias, int(groups), float(eps), act)
+    code = api._one_of(api._ACTS, act, "act")
+    api._one_of(api._OPERATOR_DTYPES, x.dtype, "the type of x")
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None and t.device != x.device:
+            raise ValueError(f"{name} must be on {x.device}, got {t.device}")
+    x = x.contiguous()
+    with api._on_device_of(x):
+        if _plain(x, weight, bias):
+            return _native_functions().norm_act(x, weight, bias, int(groups), float(eps), code)
+        return GroupNormActFunction.apply(x, weight, bias, int(groups), float(eps), act)
 
 
 class GroupNormAct(torch.nn.Module):
