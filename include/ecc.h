@@ -389,8 +389,9 @@ int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t point
  *                and gradients NaN
  *   reduction    ECC_MEAN (over the rows that are not left out; 0 where there are none), ECC_SUM, or ECC_EACH
  *   loss         device float32 out: [1], or [rows] for ECC_EACH
- *   lse          device float32 [rows] out, log sum_v exp z_iv for ecc_xent_bwd, or NULL
- *   counted      device int64 [1] out, the number of rows that are not left out, for ecc_xent_bwd; NULL with lse
+ *   stats        device double [rows][2], 16-byte aligned, out for ecc_xent_bwd, or NULL: log sum_v exp z_iv, and one minus
+ *                the label's probability
+ *   counted      device int64 [1] out, the number of rows that are not left out, for ecc_xent_bwd; NULL with stats
  * ecc_xent_bwd: grad_loss (device float32, [1] or [rows] as the loss) carried on to grad_hidden and grad_weight (as hidden
  * and weight), either of which may be NULL.  Rows that are left out get zeros and, whatever their features hold, add
  * nothing to grad_weight.
@@ -404,10 +405,10 @@ int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t point
 #define ECC_EACH 2
 size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtype dtype, int backward);
 int ecc_xent_fwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
-                 ecc_dtype dtype, int64_t ignore_index, int reduction, float* loss, float* lse, int64_t* counted,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, float* loss, double* stats, int64_t* counted,
                  void* workspace, size_t workspace_bytes, void* hip_stream);
 int ecc_xent_bwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
-                 ecc_dtype dtype, int64_t ignore_index, int reduction, const float* lse, const int64_t* counted,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, const double* stats, const int64_t* counted,
                  const float* grad_loss, void* grad_hidden, void* grad_weight, void* workspace, size_t workspace_bytes,
                  void* hip_stream);
 

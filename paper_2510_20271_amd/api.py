@@ -466,43 +466,43 @@ def _xent_args(hidden, weight, labels, reduction):
     return rows, dim, weight.shape[0], dtype, _one_of(_REDUCTIONS, reduction, "reduction")
 
 
-def ecc_xent_fwd(hidden, weight, labels, ignore_index=-100, reduction="mean", loss=None, lse=None, counted=None,
+def ecc_xent_fwd(hidden, weight, labels, ignore_index=-100, reduction="mean", loss=None, stats=None, counted=None,
                  workspace=None, keep=True):
     """Cross entropy of the linear head z = hidden weight^T: hidden [rows, dim], weight [classes, dim] (float32 / float16
-    / bfloat16, contiguous), labels int64 [rows].  Returns (loss, lse, counted): loss float32, a scalar or [rows] with
-    reduction="none"; lse [rows] and counted (an int64 scalar) are what ecc_xent_bwd needs, None with keep=False."""
-    _need_device(hidden, weight, labels, loss, lse, counted, workspace)
+    / bfloat16, contiguous), labels int64 [rows].  Returns (loss, stats, counted): loss float32, a scalar or [rows] with
+    reduction="none"; stats [rows, 2] float64 and counted (an int64 scalar) are what ecc_xent_bwd needs, None with keep=False."""
+    _need_device(hidden, weight, labels, loss, stats, counted, workspace)
     _on_current_device(hidden)
     rows, dim, classes, dtype, code = _xent_args(hidden, weight, labels, reduction)
     dev = hidden.device
     shape = (rows,) if code == ECC_EACH else ()
     _like("loss", loss, shape, torch.float32, dev)
-    _like("lse", lse, (rows,), torch.float32, dev)
+    _like("stats", stats, (rows, 2), torch.float64, dev)
     _like("counted", counted, (), torch.int64, dev)
     if loss is None:
         loss = torch.empty(shape, dtype=torch.float32, device=dev)
-    if keep and lse is None:
-        lse = torch.empty(rows, dtype=torch.float32, device=dev)
+    if keep and stats is None:
+        stats = torch.empty((rows, 2), dtype=torch.float64, device=dev)
     if keep and counted is None:
         counted = torch.empty((), dtype=torch.int64, device=dev)
     if workspace is None:
         workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, False), dev)
     _check(_lib.load().ecc_xent_fwd(_ptr(hidden), _ptr(weight), _ptr(labels), rows, dim, classes, dtype,
-                                    int(ignore_index), code, _ptr(loss), _ptr(lse), _ptr(counted), _ptr(workspace),
+                                    int(ignore_index), code, _ptr(loss), _ptr(stats), _ptr(counted), _ptr(workspace),
                                     workspace.numel(), _stream()))
-    return loss, lse, counted
+    return loss, stats, counted
 
 
-def ecc_xent_bwd(hidden, weight, labels, grad_loss, lse, counted, ignore_index=-100, reduction="mean",
+def ecc_xent_bwd(hidden, weight, labels, grad_loss, stats, counted, ignore_index=-100, reduction="mean",
                  grad_hidden=None, grad_weight=None, workspace=None, skip=()):
     """(grad_hidden, grad_weight) of ecc_xent_fwd from the upstream gradient grad_loss (float32, as the loss) and what
     it returned.  skip: the name of the output that is not wanted, if one is not."""
-    _need_device(hidden, weight, labels, grad_loss, lse, counted, grad_hidden, grad_weight, workspace)
+    _need_device(hidden, weight, labels, grad_loss, stats, counted, grad_hidden, grad_weight, workspace)
     _on_current_device(hidden)
     rows, dim, classes, dtype, code = _xent_args(hidden, weight, labels, reduction)
     dev = hidden.device
     _like("grad_loss", grad_loss, (rows,) if code == ECC_EACH else (), torch.float32, dev)
-    _like("lse", lse, (rows,), torch.float32, dev)
+    _like("stats", stats, (rows, 2), torch.float64, dev)
     _like("counted", counted, (), torch.int64, dev)
     _like("grad_hidden", grad_hidden, hidden.shape, hidden.dtype, dev)
     _like("grad_weight", grad_weight, weight.shape, weight.dtype, dev)
@@ -513,7 +513,7 @@ def ecc_xent_bwd(hidden, weight, labels, grad_loss, lse, counted, ignore_index=-
     if workspace is None:
         workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, True), dev)
     _check(_lib.load().ecc_xent_bwd(_ptr(hidden), _ptr(weight), _ptr(labels), rows, dim, classes, dtype,
-                                    int(ignore_index), code, _ptr(lse), _ptr(counted), _ptr(grad_loss),
+                                    int(ignore_index), code, _ptr(stats), _ptr(counted), _ptr(grad_loss),
                                     _ptr(grad_hidden), _ptr(grad_weight), _ptr(workspace), workspace.numel(),
                                     _stream()))
     return grad_hidden, grad_weight

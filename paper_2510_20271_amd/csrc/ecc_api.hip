@@ -591,9 +591,9 @@ static int check_xent(const ecc::XentArgs& a, int dtype, bool backward, size_t w
     return rc;
   if (a.reduction != ECC_MEAN && a.reduction != ECC_SUM && a.reduction != ECC_EACH)
     return fail(ECC_ERR_INVALID_ARG, "unknown reduction %d", a.reduction);
-  if ((rc = check_array(a.lse, "lse", 4, !backward)) != ECC_OK) return rc;
+  if ((rc = check_array(a.stats, "stats", 16, !backward)) != ECC_OK) return rc;
   if ((rc = check_array(a.counted, "counted", 8, !backward)) != ECC_OK) return rc;
-  if (!a.lse != !a.counted) return fail(ECC_ERR_INVALID_ARG, "lse and counted come together");
+  if (!a.stats != !a.counted) return fail(ECC_ERR_INVALID_ARG, "stats and counted come together");
   return check_workspace(a.ws, workspace_bytes, ecc::xent_workspace_bytes(a.rows, a.dim, a.classes, dtype, backward));
 }
 
@@ -603,23 +603,23 @@ size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtyp
 }
 
 int ecc_xent_fwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
-                 ecc_dtype dtype, int64_t ignore_index, int reduction, float* loss, float* lse, int64_t* counted,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, float* loss, double* stats, int64_t* counted,
                  void* workspace, size_t workspace_bytes, void* hip_stream) {
   ecc::XentArgs a{};
   a.h = hidden; a.w = weight; a.labels = labels; a.rows = rows; a.classes = classes; a.dim = dim;
-  a.reduction = reduction; a.ignore = ignore_index; a.loss = loss; a.lse = lse; a.counted = counted; a.ws = workspace;
+  a.reduction = reduction; a.ignore = ignore_index; a.loss = loss; a.stats = stats; a.counted = counted; a.ws = workspace;
   int rc = check_array(loss, "loss", 4);
   if (rc != ECC_OK || (rc = check_xent(a, dtype, false, workspace_bytes)) != ECC_OK) return rc;
   return device_status(ecc::launch_xent_fwd(a, dtype, static_cast<hipStream_t>(hip_stream)), "ecc_xent_fwd");
 }
 
 int ecc_xent_bwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
-                 ecc_dtype dtype, int64_t ignore_index, int reduction, const float* lse, const int64_t* counted,
+                 ecc_dtype dtype, int64_t ignore_index, int reduction, const double* stats, const int64_t* counted,
                  const float* grad_loss, void* grad_hidden, void* grad_weight, void* workspace, size_t workspace_bytes,
                  void* hip_stream) {
   ecc::XentArgs a{};
   a.h = hidden; a.w = weight; a.labels = labels; a.rows = rows; a.classes = classes; a.dim = dim;
-  a.reduction = reduction; a.ignore = ignore_index; a.lse = const_cast<float*>(lse);
+  a.reduction = reduction; a.ignore = ignore_index; a.stats = const_cast<double*>(stats);
   a.counted = const_cast<int64_t*>(counted); a.up = grad_loss; a.dh = grad_hidden; a.dw = grad_weight; a.ws = workspace;
   int rc = check_xent(a, dtype, true, workspace_bytes);
   if (rc != ECC_OK) return rc;

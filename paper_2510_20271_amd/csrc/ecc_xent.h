@@ -16,7 +16,9 @@ struct XentArgs {
   int64_t rows, classes;
   int dim, reduction;
   int64_t ignore;
-  float *loss, *lse;      // forward out: [1] or [rows]; [rows] or null.  lse: backward in
+  float* loss;            // forward out: [1] or [rows]
+  // [rows][2], forward out (or null), backward in: log sum_v exp z_iv, and 1 - p_label without a difference of near numbers
+  double* stats;
   int64_t* counted;       // [1], rows that are not left out: forward out (or null), backward in
   const float* up;        // backward: upstream gradient, [1] or [rows]
   void *dh, *dw;          // backward out, either may be null

@@ -47,13 +47,21 @@ __global__ __launch_bounds__(256) void xent_lay_kernel(const T* __restrict__ fro
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------
+// s: the sum of the exponentials under the maximum m, but the label's
 __device__ __forceinline__ void xent_row(const XentArgs& a, int64_t row, float m, double s, const float* picked, float* each) {
-  const double lse = (double)m + log(s);
-  if (a.lse) a.lse[row] = (float)lse;
   const int64_t label = a.labels[row];
-  each[row] = label == a.ignore ? 0.0f : label < 0 || label >= a.classes ? NAN : (float)(lse - (double)picked[row]);
+  const bool has = label >= 0 && label < a.classes;
+  // below the maximum, and the sum with the label's exponential; where that is most of it, log1p of the others' share keeps a small
+  // loss's digits
+  const double d = has ? (double)m - (double)picked[row] : 0.0, all = has ? s + exp(-d) : s;
+  if (a.stats) {
+    a.stats[row * 2] = (double)m + log(all);
+    a.stats[row * 2 + 1] = s / all;
+  }
+  const double loss = d < 40.0 ? log1p(s * exp(d)) : d + log(all);
+  each[row] = label == a.ignore ? 0.0f : has ? (float)loss : NAN;
 }
-// A row's tiles joined by `team` lanes (a power of two): lse, and the row's loss.
+// A row's tiles joined by `team` lanes (a power of two).
 __global__ __launch_bounds__(256) void xent_rows_kernel(XentArgs a, const float2* part, const float* picked, float* each,
                                                         int64_t parts, int team) {
   const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / team;
@@ -396,7 +404,7 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
     g.scale = scale;
     // dz of the piece
     g.a = wm; g.b = hm; g.M = count; g.N = a.rows; g.K = a.dim; g.splits = 1;
-    g.labels = a.labels; g.ignore = a.ignore; g.v0 = v0; g.lse = a.lse; g.row_scale = row_scale;
+    g.labels = a.labels; g.ignore = a.ignore; g.v0 = v0; g.stats = a.stats; g.row_scale = row_scale;
     g.dz = dz; g.dz_ld = ld; g.dz_plane = a.rows * ld;
     if ((e = launch_product<E, T>(kLogits, false, p.shape, g, st)) != hipSuccess) return e;
     if (a.dh) {

@@ -102,36 +102,36 @@ Tensor norm_act(const Tensor& x, const c10::optional<Tensor>& weight, const c10:
   return norm_forward(x, w, b, (int)groups, (float)eps, (int)act, nullptr);
 }
 
-Tensor xent_forward(const Tensor& h, const Tensor& w, const Tensor& labels, int64_t ignore, int reduction, Tensor* lse,
+Tensor xent_forward(const Tensor& h, const Tensor& w, const Tensor& labels, int64_t ignore, int reduction, Tensor* stats,
                     Tensor* counted) {
   const int64_t rows = h.size(0), classes = w.size(0);
   const int dim = (int)h.size(1);
   const auto opts = h.options().dtype(at::kFloat);
   Tensor loss = reduction == ECC_EACH ? at::empty({rows}, opts) : at::empty({}, opts);
-  if (lse) {
-    *lse = at::empty({rows}, opts);
+  if (stats) {
+    *stats = at::empty({rows, 2}, h.options().dtype(at::kDouble));
     *counted = at::empty({}, h.options().dtype(at::kLong));
   }
   const Tensor ws = room(ecc_xent_workspace_bytes(rows, dim, classes, code_of(h), 0), h);
   check(ecc_xent_fwd(h.data_ptr(), w.data_ptr(), labels.data_ptr<int64_t>(), rows, dim, classes, code_of(h), ignore, reduction,
-                     loss.data_ptr<float>(), lse ? lse->data_ptr<float>() : nullptr,
-                     lse ? counted->data_ptr<int64_t>() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream()));
+                     loss.data_ptr<float>(), stats ? stats->data_ptr<double>() : nullptr,
+                     stats ? counted->data_ptr<int64_t>() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream()));
   return loss;
 }
 
 struct Xent : public torch::autograd::Function<Xent> {
   static Tensor forward(AutogradContext* ctx, const Tensor& h, const Tensor& w, const Tensor& labels, int64_t ignore,
                         int64_t reduction) {
-    Tensor lse, counted;
-    Tensor loss = xent_forward(h, w, labels, ignore, (int)reduction, &lse, &counted);
-    ctx->save_for_backward({h, w, labels, lse, counted});
+    Tensor stats, counted;
+    Tensor loss = xent_forward(h, w, labels, ignore, (int)reduction, &stats, &counted);
+    ctx->save_for_backward({h, w, labels, stats, counted});
     ctx->saved_data["ignore"] = ignore;
     ctx->saved_data["reduction"] = reduction;
     return loss;
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
     const variable_list saved = ctx->get_saved_variables();
-    const Tensor &h = saved[0], &w = saved[1], &labels = saved[2], &lse = saved[3], &counted = saved[4];
+    const Tensor &h = saved[0], &w = saved[1], &labels = saved[2], &stats = saved[3], &counted = saved[4];
     const int64_t ignore = ctx->saved_data["ignore"].toInt();
     const int reduction = (int)ctx->saved_data["reduction"].toInt();
     const Tensor up = grads[0].contiguous().to(at::kFloat);
@@ -142,7 +142,7 @@ struct Xent : public torch::autograd::Function<Xent> {
     const int dim = (int)h.size(1);
     check_device(w, h.scalar_type(), -1, h.device());
     check_device(labels, at::kLong, rows, h.device());
-    check_device(lse, at::kFloat, rows, h.device());
+    check_device(stats, at::kDouble, rows * 2, h.device());
     check_device(counted, at::kLong, 1, h.device());
     check_device(up, at::kFloat, reduction == ECC_EACH ? rows : 1, h.device());
     Tensor dh, dw;
@@ -151,7 +151,7 @@ struct Xent : public torch::autograd::Function<Xent> {
     if (dh.defined() || dw.defined()) {
       const Tensor ws = room(ecc_xent_workspace_bytes(rows, dim, classes, code_of(h), 1), h);
       check(ecc_xent_bwd(h.data_ptr(), w.data_ptr(), labels.data_ptr<int64_t>(), rows, dim, classes, code_of(h), ignore, reduction,
-                         lse.data_ptr<float>(), counted.data_ptr<int64_t>(), up.data_ptr<float>(), at_or_null(dh),
+                         stats.data_ptr<double>(), counted.data_ptr<int64_t>(), up.data_ptr<float>(), at_or_null(dh),
                          at_or_null(dw), ws.data_ptr(), (size_t)ws.numel(), stream()));
     }
     variable_list out{dh, dw, Tensor(), Tensor(), Tensor()};

@@ -23,19 +23,19 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, labels, ignore_index: int, reduction: str):
         keep = any(ctx.needs_input_grad[:2])
-        loss, lse, counted = api.ecc_xent_fwd(hidden.detach(), weight.detach(), labels, ignore_index, reduction, keep=keep)
+        loss, stats, counted = api.ecc_xent_fwd(hidden.detach(), weight.detach(), labels, ignore_index, reduction, keep=keep)
         ctx.ignore_index, ctx.reduction = ignore_index, reduction
         if keep:
-            ctx.save_for_backward(hidden, weight, labels, lse, counted)
+            ctx.save_for_backward(hidden, weight, labels, stats, counted)
         return loss
 
     @staticmethod
     @_once
     def backward(ctx, grad_loss):
-        hidden, weight, labels, lse, counted = ctx.saved_tensors
+        hidden, weight, labels, stats, counted = ctx.saved_tensors
         skip = [n for n, need in zip(("grad_hidden", "grad_weight"), ctx.needs_input_grad) if not need]
         with api._on_device_of(hidden):
-            grads = api.ecc_xent_bwd(hidden, weight, labels, grad_loss.contiguous(), lse, counted, ctx.ignore_index,
+            grads = api.ecc_xent_bwd(hidden, weight, labels, grad_loss.contiguous(), stats, counted, ctx.ignore_index,
                                      ctx.reduction, skip=skip)
         return *grads, None, None, None
 

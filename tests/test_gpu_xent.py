@@ -95,9 +95,9 @@ def test_labels_out_of_range_are_seen():
     for bad in (-1, 30, 2 ** 40, -2 ** 60):
         lab = labels.clone()
         lab[7] = bad
-        loss, lse, counted = api.ecc_xent_fwd(h, W, lab, reduction="none")
+        loss, stats, counted = api.ecc_xent_fwd(h, W, lab, reduction="none")
         assert bool(torch.isnan(loss[7])) and torch.equal(loss[:7], good[:7]) and torch.equal(loss[8:], good[8:])
-        dh, dW = api.ecc_xent_bwd(h, W, lab, torch.ones(40, device="cuda"), lse, counted, reduction="none")
+        dh, dW = api.ecc_xent_bwd(h, W, lab, torch.ones(40, device="cuda"), stats, counted, reduction="none")
         assert bool(torch.isnan(dh[7]).all()) and bool(torch.isfinite(dh[:7]).all()) and bool(torch.isnan(dW).all())
         assert bool(torch.isnan(api.ecc_xent_fwd(h, W, lab)[0]))
 
@@ -141,10 +141,10 @@ def test_layouts(dtype):
         woff.copy_(W)
         _check(off, woff, labels, "mean", up)
         # outputs off their alignment, nothing beside them touched
-        loss, lse, counted = api.ecc_xent_fwd(off, woff, labels)
+        loss, stats, counted = api.ecc_xent_fwd(off, woff, labels)
         gh = torch.full((h.numel() + 8,), 7.0, dtype=dtype, device="cuda")
         gw = torch.full((W.numel() + 8,), 7.0, dtype=dtype, device="cuda")
-        api.ecc_xent_bwd(off, woff, labels, torch.ones((), device="cuda"), lse, counted,
+        api.ecc_xent_bwd(off, woff, labels, torch.ones((), device="cuda"), stats, counted,
                          grad_hidden=gh[shift:shift + h.numel()].view_as(h), grad_weight=gw[shift:shift + W.numel()].view_as(W))
         for t, size in ((gh, h.numel()), (gw, W.numel())):
             assert bool((t[:shift] == 7).all()) and bool((t[shift + size:] == 7).all())
@@ -153,18 +153,18 @@ def test_layouts(dtype):
 @pytest.mark.parametrize("n,d,V,dtype", [(300, 64, 900, BF16), (40, 50, 3000, F32), (3000, 32, 20, F16)])
 def test_same_bits_again_and_one_gradient_alone(n, d, V, dtype):
     h, W, labels, up = _data(n, d, V, dtype, seed=8)
-    loss, lse, counted = api.ecc_xent_fwd(h, W, labels)
+    loss, stats, counted = api.ecc_xent_fwd(h, W, labels)
     assert int(counted) == int((labels != -100).sum())
     one = torch.ones((), device="cuda")
-    dh, dW = api.ecc_xent_bwd(h, W, labels, one, lse, counted)
+    dh, dW = api.ecc_xent_bwd(h, W, labels, one, stats, counted)
     for _ in range(3):
         again = api.ecc_xent_fwd(h, W, labels)
-        assert torch.equal(loss, again[0]) and torch.equal(lse, again[1])
-        a, c = api.ecc_xent_bwd(h, W, labels, one, lse, counted)
+        assert torch.equal(loss, again[0]) and torch.equal(stats, again[1])
+        a, c = api.ecc_xent_bwd(h, W, labels, one, stats, counted)
         assert torch.equal(a, dh) and torch.equal(c, dW)
-    a, c = api.ecc_xent_bwd(h, W, labels, one, lse, counted, skip=("grad_weight",))
+    a, c = api.ecc_xent_bwd(h, W, labels, one, stats, counted, skip=("grad_weight",))
     assert torch.equal(a, dh) and c is None
-    a, c = api.ecc_xent_bwd(h, W, labels, one, lse, counted, skip=("grad_hidden",))
+    a, c = api.ecc_xent_bwd(h, W, labels, one, stats, counted, skip=("grad_hidden",))
     assert a is None and torch.equal(c, dW)
 
 
@@ -202,8 +202,8 @@ def test_on_a_stream_of_its_own_and_in_graphs():
     one = torch.ones((), device="cuda")
 
     def step(hi):
-        loss, lse, counted = api.ecc_xent_fwd(hi, W, labels)
-        return (loss, *api.ecc_xent_bwd(hi, W, labels, one, lse, counted))
+        loss, stats, counted = api.ecc_xent_fwd(hi, W, labels)
+        return (loss, *api.ecc_xent_bwd(hi, W, labels, one, stats, counted))
     want = step(h)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
@@ -239,10 +239,38 @@ def test_refusals():
                  lambda: linear_cross_entropy(h, W, labels.int()), lambda: linear_cross_entropy(h, W, labels, reduction="max"),
                  lambda: linear_cross_entropy(h.double(), W.double(), labels),
                  lambda: api.ecc_xent_fwd(h.t().contiguous().t(), W, labels),
-                 lambda: api.ecc_xent_bwd(h, W, labels, torch.ones(6, device="cuda"), torch.zeros(6, device="cuda"),
+                 lambda: api.ecc_xent_bwd(h, W, labels, torch.ones(6, device="cuda"), torch.zeros(6, 2, dtype=torch.float64, device="cuda"),
                                           torch.ones((), dtype=torch.int64, device="cuda"))):
         with pytest.raises(ValueError):
             call()
     with pytest.raises(api.EccError) as e:
         api.ecc_xent_fwd(h, W, labels, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     assert e.value.status == -3
+
+
+def test_small_losses_keep_their_digits():
+    """Rows that are almost sure of their label: loss = log(1 + r) with r from 1e-2 down to 1e-9, and the gradient -r / (1 + r).
+    The logits are exact in float32 (powers of two), so what is left is the exponential's and a few roundings: 40 E."""
+    n, d = 28, 32
+    h = torch.zeros(n, d, device="cuda")
+    h[:, 0] = 1.0
+    gap = torch.arange(4, 18, 0.5)
+    W = torch.zeros(n + 1, d, device="cuda")
+    W[:n, 0] = gap.cuda()
+    for i in range(n):  # one row at a time: class i leads by gap[i] over n others at 0
+        lone = torch.zeros(n + 1, d, device="cuda")
+        lone[3, 0] = gap[i]
+        label = torch.tensor([3], device="cuda")
+        loss, stats, counted = api.ecc_xent_fwd(h[i:i + 1], lone, label, reduction="none")
+        r = n * float(torch.exp(-gap[i].double()))
+        assert abs(float(loss) / float(torch.log1p(torch.tensor(r, dtype=torch.float64))) - 1) < 40 * 2.0 ** -24
+        dh, _ = api.ecc_xent_bwd(h[i:i + 1], lone, label, torch.ones(1, device="cuda"), stats, counted, reduction="none",
+                                 skip=("grad_weight",))
+        assert abs(float(dh[0, 0]) / (-r / (1 + r) * float(gap[i])) - 1) < 40 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_tiles(dtype):
+    """Enough rows, classes and features for the largest tiles of all three products, ragged in each."""
+    h, W, labels, up = _data(2300, 1032 if dtype == BF16 else 520, 9001, dtype, seed=12)
+    _check(h, W, labels, "mean", up)

@@ -65,7 +65,7 @@ def test_norm_rejects_what_one_direction_needs():
 
 
 def _xent(**kw):
-    a = dict(h=FAKE, w=FAKE, labels=FAKE, rows=4, dim=8, classes=16, dtype=2, ignore=-100, reduction=0, loss=FAKE, lse=FAKE,
+    a = dict(h=FAKE, w=FAKE, labels=FAKE, rows=4, dim=8, classes=16, dtype=2, ignore=-100, reduction=0, loss=FAKE, stats=FAKE,
              counted=FAKE, ws=FAKE, ws_bytes=1 << 30)
     a.update(kw)
     return a
@@ -73,12 +73,12 @@ def _xent(**kw):
 
 def _xent_fwd(a):
     return _lib.load().ecc_xent_fwd(a["h"], a["w"], a["labels"], a["rows"], a["dim"], a["classes"], a["dtype"], a["ignore"],
-                                    a["reduction"], a["loss"], a["lse"], a["counted"], a["ws"], a["ws_bytes"], None)
+                                    a["reduction"], a["loss"], a["stats"], a["counted"], a["ws"], a["ws_bytes"], None)
 
 
 def _xent_bwd(a, up=FAKE, gh=FAKE, gw=FAKE):
     return _lib.load().ecc_xent_bwd(a["h"], a["w"], a["labels"], a["rows"], a["dim"], a["classes"], a["dtype"], a["ignore"],
-                                    a["reduction"], a["lse"], a["counted"], up, gh, gw, a["ws"], a["ws_bytes"], None)
+                                    a["reduction"], a["stats"], a["counted"], up, gh, gw, a["ws"], a["ws_bytes"], None)
 
 
 @pytest.mark.parametrize("kw,status,word", [
@@ -87,8 +87,8 @@ def _xent_bwd(a, up=FAKE, gh=FAKE, gw=FAKE):
     (dict(rows=1 << 31), UNSUPPORTED, "2^31"), (dict(classes=1 << 31), UNSUPPORTED, "2^31"),
     (dict(dim=1 << 17), UNSUPPORTED, "dim"), (dict(dtype=1), INVALID, "dtype"), (dict(reduction=3), INVALID, "reduction"),
     (dict(h=ctypes.c_void_p(0x1002)), INVALID, "aligned"), (dict(w=ODD), INVALID, "aligned"),
-    (dict(labels=ctypes.c_void_p(0x1004)), INVALID, "aligned"), (dict(lse=None), INVALID, "lse"),
-    (dict(counted=None), INVALID, "counted"), (dict(lse=ODD), INVALID, "aligned"),
+    (dict(labels=ctypes.c_void_p(0x1004)), INVALID, "aligned"), (dict(stats=None), INVALID, "stats"),
+    (dict(counted=None), INVALID, "counted"), (dict(stats=ctypes.c_void_p(0x1008)), INVALID, "aligned"),
     (dict(counted=ctypes.c_void_p(0x1004)), INVALID, "aligned"), (dict(ws=None), WORKSPACE, "workspace"),
     (dict(ws_bytes=8), WORKSPACE, "workspace"), (dict(ws=ctypes.c_void_p(0x1010)), WORKSPACE, "aligned"),
 ])
