@@ -8,6 +8,7 @@
 #include "ecc_xent.h"
 
 #include <algorithm>
+#include <numeric>
 
 #include "ecc_xent_product.h"
 
@@ -21,11 +22,17 @@ static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 static int64_t up_to(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 
 // ---- operands --------------------------------------------------------------------------------------------------------------
-// rows of `dim` elements laid out as the products take them: [planes][rows][ld], zeros behind a row's end
+// One operand to be laid out as the products take them: [planes][rows][ld], zeros behind a row's end.  blocks: 0 where the
+// caller's own memory will do.
+struct Lay {
+  const void* from;
+  unsigned short* to;
+  int64_t rows, blocks;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void xent_lay_kernel(const T* __restrict__ from, int64_t rows, int dim, int ld,
-                                                       unsigned short* __restrict__ to) {
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, all = rows * ld;
+__device__ __forceinline__ void lay_chunk(const Lay& l, int dim, int ld, int64_t block) {
+  const T* from = static_cast<const T*>(l.from);
+  const int64_t at = (block * 256 + threadIdx.x) * 8, all = l.rows * ld;
   if (at >= all) return;
   const int64_t row = at / ld;
   const int k = (int)(at - row * ld);
@@ -42,13 +49,13 @@ __global__ __launch_bounds__(256) void xent_lay_kernel(const T* __restrict__ fro
     w.y = (unsigned)s[2][p] | (unsigned)s[3][p] << 16;
     w.z = (unsigned)s[4][p] | (unsigned)s[5][p] << 16;
     w.w = (unsigned)s[6][p] | (unsigned)s[7][p] << 16;
-    *reinterpret_cast<uint4*>(to + p * all + at) = w;
+    *reinterpret_cast<uint4*>(l.to + p * all + at) = w;
   }
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------
 // s: the sum of the exponentials under the maximum m, but the label's
-__device__ __forceinline__ void xent_row(const XentArgs& a, int64_t row, float m, double s, const float* picked, float* each) {
+__device__ __forceinline__ float xent_row(const XentArgs& a, int64_t row, float m, double s, const float* picked, float* each) {
   const int64_t label = a.labels[row];
   const bool has = label >= 0 && label < a.classes;
   // below the maximum, and the sum with the label's exponential; where that is most of it, log1p of the others' share keeps a small
@@ -59,7 +66,7 @@ __device__ __forceinline__ void xent_row(const XentArgs& a, int64_t row, float m
     a.stats[row * 2 + 1] = s / all;
   }
   const double loss = d < 40.0 ? log1p(s * exp(d)) : d + log(all);
-  each[row] = label == a.ignore ? 0.0f : has ? (float)loss : NAN;
+  return each[row] = label == a.ignore ? 0.0f : has ? (float)loss : NAN;
 }
 // A row's tiles joined by `team` lanes (a power of two).
 __global__ __launch_bounds__(256) void xent_rows_kernel(XentArgs a, const float2* part, const float* picked, float* each,
@@ -134,6 +141,47 @@ __global__ __launch_bounds__(kSumThreads) void xent_sum_kernel(XentArgs a, const
   if (gridDim.x == 1) xent_finish(a, sum[0], count[0]);
   else out[blockIdx.x] = {sum[0], count[0]};
 }
+// Everything behind the sums in one block, where there is little of it: the rows, then the loss.
+__global__ __launch_bounds__(kSumThreads) void xent_short_kernel(XentArgs a, const float2* part, const float* picked, float* each,
+                                                                 int64_t parts, int team) {
+  __shared__ double sum[kSumThreads / 64];
+  __shared__ long long count[kSumThreads / 64];
+  const int lane = threadIdx.x & (team - 1), step = kSumThreads / team;
+  double loss = 0.0;
+  long long n = 0;
+  for (int64_t r0 = 0; r0 < a.rows; r0 += step) {  // (block-uniform)
+    const int64_t row = r0 + threadIdx.x / team;
+    const bool in = row < a.rows;
+    const float2* p = part + (in ? row : 0) * parts;
+    float m = -INFINITY;
+    for (int64_t t = lane; t < parts; t += team) m = fmaxf(m, p[t].x);
+    for (int o = team / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    double s = 0.0;
+    for (int64_t t = lane; t < parts; t += team) s += (double)p[t].y * (p[t].x == m ? 1.0 : (double)__expf(p[t].x - m));
+    for (int o = team / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (in && lane == 0) {
+      loss += (double)xent_row(a, row, m, s, picked, each);
+      n += a.labels[row] != a.ignore;
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    loss += __shfl_xor(loss, o);
+    n += __shfl_xor(n, o);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    sum[threadIdx.x >> 6] = loss;
+    count[threadIdx.x >> 6] = n;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  loss = 0.0;
+  n = 0;
+  for (int k = 0; k < kSumThreads / 64; ++k) {
+    loss += sum[k];
+    n += count[k];
+  }
+  xent_finish(a, loss, n);
+}
 __global__ __launch_bounds__(64) void xent_total_kernel(XentArgs a, const RowSum* part, int blocks) {
   double s = 0.0;
   long long n = 0;
@@ -163,13 +211,20 @@ __global__ __launch_bounds__(kSumThreads) void xent_top_kernel(const float* up, 
 }
 
 // What each row's dz is multiplied by, which rows count, and what the products are multiplied by.
-__global__ __launch_bounds__(256) void xent_scale_kernel(XentArgs a, bool half, const float* top, float* row_scale,
-                                                         unsigned long long* keep, float* scale) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  float by = half ? kHalfScale : 1.0f, back = 1.0f / by;
+struct Scales {
+  const float* top;  // float16 with a gradient for each row: the largest of them
+  float* row_scale;
+  unsigned long long* keep;
+  float* scale;
+  bool half;
+  int64_t blocks;  // 0: none wanted
+};
+__device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, int64_t block) {
+  const int64_t i = block * 256 + threadIdx.x;
+  float by = c.half ? kHalfScale : 1.0f, back = 1.0f / by;
   if (a.reduction == kEach) {
-    if (half) {
-      const float t = top[0] > 0.0f ? top[0] : 1.0f;
+    if (c.half) {
+      const float t = c.top[0] > 0.0f ? c.top[0] : 1.0f;
       by /= t;
       back *= t;
     }
@@ -183,11 +238,21 @@ __global__ __launch_bounds__(256) void xent_scale_kernel(XentArgs a, bool half, 
     counts = label != a.ignore;
     float v = a.reduction == kEach ? a.up[i] * by : by;
     if (counts && (label < 0 || label >= a.classes)) v = NAN;
-    row_scale[i] = v;
+    c.row_scale[i] = v;
   }
   const unsigned long long bits = __ballot(counts);
-  if ((threadIdx.x & 63) == 0 && i < a.rows) keep[i / 64] = bits;
-  if (i == 0) scale[0] = back;
+  if ((threadIdx.x & 63) == 0 && i < a.rows) c.keep[i / 64] = bits;
+  if (i == 0) c.scale[0] = back;
+}
+
+// What comes before the products, in one launch: both operands laid out and the rows' scales, a run of blocks each.
+template <typename T>
+__global__ __launch_bounds__(256) void xent_prepare_kernel(XentArgs a, Lay h, Lay w, int ld, Scales c) {
+  int64_t block = blockIdx.x;
+  if (block < h.blocks) return lay_chunk<T>(h, a.dim, ld, block);
+  block -= h.blocks;
+  if (block < w.blocks) return lay_chunk<T>(w, a.dim, ld, block);
+  scale_rows(a, c, block - w.blocks);
 }
 
 // out = narrow(scale * sum of the splits), `team` threads to an element, added in a fixed order
@@ -218,7 +283,7 @@ __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int sp
 }
 
 // ---- plans -----------------------------------------------------------------------------------------------------------------
-constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of dz, and of laid-out weights: what the Infinity Cache holds
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of a plane of dz, and of laid-out weights: what the Infinity Cache holds
 constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
 constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 
@@ -258,15 +323,20 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   XentPlan p{};
   const int P = planes_of(dtype);
   const int64_t ld = ld_of(dim);
-  const auto pieces = [&](int64_t most) {  // equal pieces of multiples of 256 classes, at most `most`
+  // Pieces of at most `most` classes, equal ones.  Where the last piece is small anyway the others hold whole rounds of 256 large
+  // tiles (2048 rows, 50021 classes: 32768 and 17253, 4 + 3 rounds of blocks; halves: 4 + 4).
+  const auto pieces = [&](int64_t most) {
     most = std::max<int64_t>(256, most / 256 * 256);
     const int64_t count = (classes + most - 1) / most;
-    return std::min(classes, up_to((classes + count - 1) / count, 256));
+    if (count == 1) return classes;
+    const int64_t tiles_n = (rows + 255) / 256, round = 256 / std::gcd<int64_t>(256, tiles_n) * 256;
+    if (most / round * round * count >= classes) return most / round * round;
+    return up_to((classes + count - 1) / count, 256);
   };
   p.fwd_shape = shape_of(classes, rows, 1);
   p.parts = (classes + kPlans[p.fwd_shape].bm - 1) / kPlans[p.fwd_shape].bm * kPlans[p.fwd_shape].wm;
-  p.fwd_piece = pieces(std::min(kPieceMost * 8, kPieceBytes / (ld * 2 * P)));
-  p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * 2 * P), dtype == kF32 ? kPieceBytes / (ld * 2 * P) : kPieceMost}));
+  p.fwd_piece = pieces(std::min(kPieceMost * 8, kPieceBytes / (ld * 2)));
+  p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * 2), dtype == kF32 ? kPieceBytes / (ld * 2) : kPieceMost}));
   p.ld_dz = up_to(p.piece, 8);
   p.shape = shape_of(p.piece, rows, 1);
   const int64_t long_k = std::max<int64_t>(1, p.piece / kDepth / 16), long_n = std::max<int64_t>(1, rows / kDepth / 16);
@@ -308,14 +378,17 @@ struct Room {  // hands out a workspace
 // Whether the products can read the caller's own memory: 16-bit elements, rows of whole 16-byte chunks.
 static bool as_it_is(const void* p, int dim, int dtype) { return dtype != kF32 && dim % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-template <typename T>
-static Matrix laid(const T* from, int64_t rows, int dim, void* room, bool own, hipStream_t st) {
-  if (own) return {from, rows, dim, 0};
+// An operand as the products see it, and what has to be laid out for that.
+static Matrix laid(const void* from, int64_t rows, int dim, void* room, bool own, Lay* l) {
   const int ld = ld_of(dim);
-  const int64_t chunks = rows * ld / 8;
-  hipLaunchKernelGGL(xent_lay_kernel<T>, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, from, rows, dim, ld,
-                     static_cast<unsigned short*>(room));
+  *l = {from, static_cast<unsigned short*>(room), rows, own ? 0 : (rows * ld / 8 + 255) / 256};
+  if (own) return {from, rows, dim, 0};
   return {room, rows, ld, rows * ld};
+}
+template <typename T>
+static void prepare(const XentArgs& a, const Lay& h, const Lay& w, const Scales& c, hipStream_t st) {
+  const int64_t blocks = h.blocks + w.blocks + c.blocks;
+  if (blocks) hipLaunchKernelGGL(xent_prepare_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, a, h, w, ld_of(a.dim), c);
 }
 
 // T: element type of the arguments, E: of the products' operands
@@ -331,7 +404,8 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   if (a.reduction == kEach) each = a.loss;
   const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
   ProductArgs g{};
-  g.b = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), st);
+  Lay lh, lw;
+  g.b = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), &lh);
   g.N = a.rows;
   g.K = a.dim;
   g.splits = 1;
@@ -347,18 +421,24 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   hipError_t e = hipSuccess;
   for (int64_t v0 = 0; v0 < a.classes && e == hipSuccess; v0 += piece) {
     const int64_t count = std::min(piece, a.classes - v0);
-    g.a = laid(w + v0 * a.dim, count, a.dim, lay_w, own, st);
+    g.a = laid(w + v0 * a.dim, count, a.dim, lay_w, own, &lw);
+    prepare<T>(a, lh, lw, Scales{}, st);
+    lh.blocks = 0;
     g.M = count;
     g.v0 = v0;
     g.part0 = v0 / plan.bm * plan.wm;
     e = launch_product<E, T>(kLogits, true, p.fwd_shape, g, st);
   }
   if (e != hipSuccess) return e;
+  int team = 64;
+  while (team > 1 && team / 2 >= p.parts) team /= 2;
+  if (p.parts <= 512 && a.rows * (p.parts + 8) <= 16384) {
+    hipLaunchKernelGGL(xent_short_kernel, dim3(1), dim3(kSumThreads), 0, st, a, part, picked, each, p.parts, team);
+    return hipGetLastError();
+  }
   if (a.rows < 512 && p.parts > 512) {
     hipLaunchKernelGGL(xent_long_row_kernel, dim3((unsigned)a.rows), dim3(1024), 0, st, a, part, picked, each, p.parts);
   } else {
-    int team = 64;
-    while (team > 1 && team / 2 >= p.parts) team /= 2;
     hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, part, picked, each,
                        p.parts, team);
   }
@@ -391,14 +471,16 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   const bool half = dtype == kF16;
   if (half && a.reduction == kEach)
     hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a.up, a.rows, scale + 1);
-  hipLaunchKernelGGL(xent_scale_kernel, dim3((unsigned)((a.rows + 255) / 256)), dim3(256), 0, st, a, half, scale + 1, row_scale,
-                     keep, scale);
-  const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), st);
+  Scales scales{scale + 1, row_scale, keep, scale, half, (a.rows + 255) / 256};
+  Lay lh, lw;
+  const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), &lh);
   const bool own = as_it_is(w, a.dim, dtype);
   hipError_t e = hipSuccess;
   for (int64_t v0 = 0; v0 < a.classes; v0 += p.piece) {
     const int64_t count = std::min(p.piece, a.classes - v0), ld = up_to(count, 8);
-    const Matrix wm = laid(w + v0 * a.dim, count, a.dim, lay_w, own, st);
+    const Matrix wm = laid(w + v0 * a.dim, count, a.dim, lay_w, own, &lw);
+    prepare<T>(a, lh, lw, scales, st);
+    lh.blocks = scales.blocks = 0;
     const Matrix zm{dz, a.rows, ld, a.rows * ld};
     ProductArgs g{};
     g.scale = scale;

@@ -1,25 +1,37 @@
 // Instances of the product kernels for one pair of element types (included by the ecc_xent_*.hip files).
 #pragma once
+#include <atomic>
+
 #include "ecc_xent_product.h"
 
 namespace ecc {
 
+template <auto KERNEL, int SHARED>
+static hipError_t product_go(const ProductArgs& g, int threads, hipStream_t st) {
+  if (SHARED > 64 << 10) {  // (told once for each kernel and device)
+    static std::atomic<uint64_t> told{0};
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (device > 63 || !(told.load(std::memory_order_relaxed) & bit)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, SHARED);
+      if (e != hipSuccess) return e;
+      told.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  hipLaunchKernelGGL(KERNEL, dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3((unsigned)threads), SHARED, st, g);
+  return hipGetLastError();
+}
+
 template <typename T, typename O, int BM, int BN, int WM, int WN, int STAGES>
 static hipError_t product_shape(int kind, bool forward, const ProductArgs& g, hipStream_t st) {
-  constexpr int kShared = STAGES * (BM + BN) * kDepth * 2;
-  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * g.splits)), block(WM * WN * 64);
-  const auto go = [&](auto kernel) -> hipError_t {
-    if (kShared > 64 << 10) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kShared);
-      if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL(kernel, grid, block, kShared, st, g);
-    return hipGetLastError();
-  };
-  if (kind == kLogits) return forward ? go(product_kernel<T, O, kLogits, true, BM, BN, WM, WN, STAGES>)
-                                      : go(product_kernel<T, O, kLogits, false, BM, BN, WM, WN, STAGES>);
-  if (kind == kHidden) return go(product_kernel<T, O, kHidden, false, BM, BN, WM, WN, STAGES>);
-  return go(product_kernel<T, O, kWeight, false, BM, BN, WM, WN, STAGES>);
+  constexpr int kShared = STAGES * (BM + BN) * kDepth * 2, kThreads = WM * WN * 64;
+  if (kind == kLogits)
+    return forward ? product_go<product_kernel<T, O, kLogits, true, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st)
+                   : product_go<product_kernel<T, O, kLogits, false, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kHidden) return product_go<product_kernel<T, O, kHidden, false, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  return product_go<product_kernel<T, O, kWeight, false, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
 }
 
 template <typename T, typename O>
