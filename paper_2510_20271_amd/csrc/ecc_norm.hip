@@ -92,34 +92,42 @@ struct NormLane {
   }
 };
 
-// Count, mean and squares of a group, joined by `team` lanes of a wave (a power of two).  Entries are [lanes][width], `per` to
-// a thread, each standing for `unit` values a row; those of the group are first .. first + len - 1 of every lane, and again at
-// every `again` (rows that hold the channels several times; 0: once).
+// the largest power of two that is at most n (n >= 1), and at most `most` (a power of two)
+__device__ __forceinline__ int power_below(int n, int most) {
+  const int p = 1 << (31 - __clz(n));
+  return p < most ? p : most;
+}
+
+// Count, mean and squares of a group, joined by `team` lanes of a wave (a power of two).  Entries are [lanes][width], 1 << shift
+// to a thread, each standing for `unit` values a row; those of the group are first .. first + len - 1 of every lane, and again
+// `repeats` times at every `again` (rows that hold the channels several times).
 __device__ __forceinline__ Moments join_entries(const double* mean, const float* m2, const int* cnt, int wide, int lanes,
-                                                int width, int first, int len, int again, int per, int unit, int team) {
-  const int lane = threadIdx.x & (team - 1);
-  const int repeats = again > 0 ? width / again : 1, row = repeats * len;
+                                                int width, int first, int len, int again, int repeats, int shift, int unit,
+                                                int team) {
+  const int lane = threadIdx.x & (team - 1), kt = power_below(len, team), rt = team / kt, l0 = lane / kt, k0 = lane & (kt - 1);
   double n = 0.0, s = 0.0;
-  for (int i = lane; i < lanes * row; i += team) {
-    const int rl = i / row, k = i - rl * row, at = (k / len) * again + first + k % len;
-    const double c = (double)(cnt[rl * wide + at / per] * unit);
-    n += c;
-    if (c > 0.0) s += c * mean[rl * width + at];
-  }
+  for (int rl = l0; rl < lanes; rl += rt)
+    for (int rep = 0, at0 = first; rep < repeats; ++rep, at0 += again)
+      for (int k = k0; k < len; k += kt) {
+        const double c = (double)(cnt[rl * wide + ((at0 + k) >> shift)] * unit);
+        n += c;
+        if (c > 0.0) s += c * mean[rl * width + at0 + k];
+      }
   for (int o = team / 2; o > 0; o >>= 1) {
     n += __shfl_xor(n, o);
     s += __shfl_xor(s, o);
   }
   const double mu = n > 0.0 ? s / n : 0.0;
   double q = 0.0;
-  for (int i = lane; i < lanes * row; i += team) {
-    const int rl = i / row, k = i - rl * row, at = (k / len) * again + first + k % len;
-    const double c = (double)(cnt[rl * wide + at / per] * unit);
-    if (c > 0.0) {
-      const double d = mean[rl * width + at] - mu;
-      q += (double)m2[rl * width + at] + c * d * d;
-    }
-  }
+  for (int rl = l0; rl < lanes; rl += rt)
+    for (int rep = 0, at0 = first; rep < repeats; ++rep, at0 += again)
+      for (int k = k0; k < len; k += kt) {
+        const double c = (double)(cnt[rl * wide + ((at0 + k) >> shift)] * unit);
+        if (c > 0.0) {
+          const double d = mean[rl * width + at0 + k] - mu;
+          q += (double)m2[rl * width + at0 + k] + c * d * d;
+        }
+      }
   for (int o = team / 2; o > 0; o >>= 1) q += __shfl_xor(q, o);
   return {n, mu, q};
 }
@@ -149,9 +157,9 @@ struct Column {
     }
     ++n;
   }
-  __device__ __forceinline__ double mean(int i) const { return (double)k[i] + (double)s[i] / (double)n; }
-  __device__ __forceinline__ float m2(int i) const {
-    const float v = q[i] - s[i] * s[i] / (float)n;
+  __device__ __forceinline__ double mean(int i, double by) const { return (double)k[i] + (double)s[i] * by; }  // by: 1 / n
+  __device__ __forceinline__ float m2(int i, float by) const {
+    const float v = q[i] - s[i] * s[i] * by;
     return v < 0.0f ? 0.0f : v;  // (a NaN stays one)
   }
 };
@@ -174,10 +182,11 @@ __device__ __forceinline__ void block_moments(const Column<V>& col, const NormGe
   if (l.on && col.n > 0) {
     double mu[V];
     float m2[V];
+    const double by = 1.0 / (double)col.n;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      mu[i] = col.mean(i);
-      m2[i] = col.m2(i);
+      mu[i] = col.mean(i, by);
+      m2[i] = col.m2(i, (float)by);
     }
 #pragma unroll
     for (int step = 1; step < V; step *= 2) {  // runs of `step` values joined in pairs
@@ -200,17 +209,17 @@ __device__ __forceinline__ void block_moments(const Column<V>& col, const NormGe
   }
   __syncthreads();
   // entries of a lane: its columns in order, `per` each; channel c0 is entry 0.  Groups of few entries share a wave.
-  const int width = geo.wide * per, again = geo.passes > 1 ? 0 : geo.channels / unit;
+  const int width = geo.wide * per, again = geo.channels / unit, repeats = geo.passes > 1 ? 1 : width / again;
   const int g0 = c0 / Cg, g1 = (cend - 1) / Cg;
-  const int most = geo.lanes * (again ? width / again : 1) * ((Cg + unit - 1) / unit);
+  const int most = geo.lanes * repeats * ((Cg + unit - 1) / unit), shift = 31 - __clz(per);
   int team = 64;
   while (team > 1 && team / 2 >= most) team /= 2;
   const int teams = (int)blockDim.x / team;
   for (int gb = g0; gb <= g1; gb += teams) {  // (whole waves take part: a team without a group repeats the last one's)
     const int g = min(gb + t / team, g1);
     const int lo = max(g * Cg, c0), hi = min((g + 1) * Cg, cend);
-    const Moments m = join_entries(e_mean, e_m2, e_cnt, geo.wide, geo.lanes, width, (lo - c0) / unit, (hi - lo) / unit, again, per,
-                                   unit, team);
+    const Moments m = join_entries(e_mean, e_m2, e_cnt, geo.wide, geo.lanes, width, (lo - c0) / unit, (hi - lo) / unit, again,
+                                   repeats, shift, unit, team);
     if ((t & (team - 1)) == 0 && gb + t / team <= g1) done(g, m);
   }
 }
@@ -560,13 +569,17 @@ __global__ __launch_bounds__(kJoinThreads) void norm_groups_kernel(NormArgs a, c
   const int64_t n = n0 + blockIdx.x / a.G;
   const float* p = part + n * parts * 2 * a.C + (int64_t)g * Cg;
   double s1 = 0.0, s2 = 0.0;
-  const int64_t all = (int64_t)parts * Cg;
-  for (int64_t i = threadIdx.x; i < all; i += kJoinThreads) {
-    const int64_t r = i / Cg;
-    const int c = (int)(i - r * Cg);
+  const int kt = power_below(Cg, kJoinThreads), rt = kJoinThreads / kt;
+  for (int c = threadIdx.x & (kt - 1); c < Cg; c += kt) {
     const double w = a.w ? (double)a.w[g * Cg + c] : 1.0;
-    s1 += w * (double)p[r * 2 * a.C + c];
-    s2 += w * (double)p[(r * 2 + 1) * a.C + c];
+    double u1 = 0.0, u2 = 0.0;
+#pragma unroll 4
+    for (int64_t r = threadIdx.x / kt; r < parts; r += rt) {
+      u1 += (double)p[r * 2 * a.C + c];
+      u2 += (double)p[(r * 2 + 1) * a.C + c];
+    }
+    s1 += w * u1;
+    s2 += w * u2;
   }
   block_add(s1, s2, room);
   if (threadIdx.x == 0) {
@@ -793,6 +806,7 @@ __global__ __launch_bounds__(kNormFused) void norm_fused_bwd_kernel(NormArgs a, 
 }
 
 // ---- plans ---------------------------------------------------------------------------------------------------------------
+constexpr int64_t kNormFew = 256;      // blocks of a sweep: one a compute unit
 constexpr int64_t kNormBlocks = 1024;  // of a sweep, about: what the card holds at a time (2048: 924 us for 907, above)
 
 // elements a vector may have: 16 bytes' worth, or fewer where an item's size or an address does not allow it
@@ -804,13 +818,16 @@ static int norm_vector(const NormArgs& a, int size) {
   return V;
 }
 
-// Rows of a block: enough blocks over `items` items for the card, four vectors a thread or more where they allow it.
+// Rows of a block.  What a block does beside its rows -- scales, the joining of its sums -- is as much as some ten rows, so
+// threads take 16 of them; fewer (four at the least) where 16 would leave compute units without a block.  (2 x 83193 x 44 in
+// float32 with four rows a thread: sums 28.7 us, second sweep 20.0; a thread takes NORM_AFTER.)
 static void share_rows(NormGeo& g, int64_t items) {
   g.lanes = (int)std::max<int64_t>(1, std::min<int64_t>(kNormThreads / g.wide, g.rows));
-  const int64_t least = (g.rows + (int64_t)g.lanes * kNormRows - 1) / ((int64_t)g.lanes * kNormRows);
-  const int64_t most = std::max<int64_t>(1, (g.rows + (int64_t)g.lanes * 4 - 1) / ((int64_t)g.lanes * 4));
-  const int64_t parts = std::max(least, std::min(most, kNormBlocks / std::max<int64_t>(1, items * g.passes)));
-  g.per = (g.rows + std::max<int64_t>(parts, 1) - 1) / std::max<int64_t>(parts, 1);
+  const auto parts_of = [&](int64_t each) { return std::max<int64_t>(1, (g.rows + g.lanes * each - 1) / (g.lanes * each)); };
+  const int64_t over = std::max<int64_t>(1, items * g.passes);
+  int64_t parts = std::max(parts_of(16), std::min(parts_of(4), kNormFew / over));
+  parts = std::max(parts_of(kNormRows), std::min(parts, std::max<int64_t>(1, kNormBlocks / over)));
+  g.per = (g.rows + parts - 1) / parts;
   g.per = (g.per + g.lanes - 1) / g.lanes * g.lanes;
   g.parts = (int)((g.rows + g.per - 1) / g.per);
 }

@@ -107,6 +107,55 @@ __global__ __launch_bounds__(1024) void xent_long_row_kernel(XentArgs a, const f
   xent_row(a, row, m, s, picked, each);
 }
 
+// Logits whose sums were split (few tiles, long rows of features): a row's maximum and sum, as a tile's epilogue leaves them ...
+__global__ __launch_bounds__(256) void xent_fold_kernel(XentArgs a, const float* sums, int splits, float2* part, float* picked, int team) {
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / team;
+  const int lane = threadIdx.x & (team - 1);
+  const bool in = row < a.rows;
+  const int64_t all = a.rows * a.classes, label = in ? a.labels[row] : -1;
+  const float* z = sums + (in ? row : 0) * a.classes;
+  float m = -INFINITY, s = 0.0f;
+  for (int64_t v = lane; v < a.classes; v += team) {
+    float x = z[v];
+    for (int k = 1; k < splits; ++k) x += z[k * all + v];
+    if (in && v == label) picked[row] = x;
+    const float top = fmaxf(m, x), base = top == -INFINITY ? 0.0f : top;
+    s = s * __expf(m - base) + (v == label ? 0.0f : __expf(x - base));
+    m = top;
+  }
+  for (int o = team / 2; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o), top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+    s = s * __expf(m - base) + s2 * __expf(m2 - base);
+    m = top;
+  }
+  if (in && lane == 0) part[row] = make_float2(m, s);
+}
+// ... or their gradient, [planes][rows][ld], for `count` classes from v0
+template <typename E, int PLANES>
+__global__ __launch_bounds__(256) void xent_dz_kernel(XentArgs a, const float* sums, int splits, int64_t v0, int64_t count, int64_t ld,
+                                                      const float* row_scale, unsigned short* dz) {
+  const int64_t all = a.rows * ld, n = a.rows * count;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / ld, v = i - row * ld, label = a.labels[row];
+    float f = 0.0f;
+    if (v < count && label != a.ignore) {
+      float x = sums[row * count + v];
+      for (int k = 1; k < splits; ++k) x += sums[k * n + row * count + v];
+      const double lse = a.stats[row * 2];
+      const float high = (float)lse, low = (float)(lse - (double)high);
+      f = (v0 + v == label ? -(float)a.stats[row * 2 + 1] : __expf((x - high) - low)) * row_scale[row];
+    }
+    if constexpr (PLANES == 1) {
+      dz[i] = __builtin_bit_cast(unsigned short, narrow<E>(f));
+    } else {
+      unsigned short p[3];
+      split3(f, p);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) dz[k * all + i] = p[k];
+    }
+  }
+}
+
 // Sum of the rows' losses and their count, a run of rows a block; one block: the loss itself.
 struct RowSum { double sum; long long count; };
 constexpr int kSumThreads = 1024;
@@ -290,13 +339,15 @@ constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 static int planes_of(int dtype) { return dtype == kF32 ? 3 : 1; }
 static int ld_of(int dim) { return (int)up_to(dim, 8); }
 
-// Tiles of 256 x 256 where they fill the card (one block a CU), of 128 x 128 otherwise; thin products have thin tiles.
-static int shape_of(int64_t M, int64_t N, int64_t runs) {
+// Tiles of 256 x 256 where they fill the card (one block a CU) and the summed axis is eight turns or more; of 128 x 128
+// otherwise, two blocks a CU, so that one's start and end run beside the other's products.  Thin products have thin tiles.
+// (385475 x 18 x 599 in float16, one turn: logits 228 us by large tiles, XENT_AFTER by the others.)
+static int shape_of(int64_t M, int64_t N, int64_t runs, int64_t turns) {
   if (N <= 32) return 2;
   if (M <= 32) return 3;
   if (M <= 64 && N > 128) return 4;
   const int64_t large = (M + 255) / 256 * ((N + 255) / 256);
-  return M > 128 && N > 128 && large * runs >= 256 ? 0 : 1;
+  return M > 128 && N > 128 && turns >= 8 && large * runs >= 256 ? 0 : 1;
 }
 // The summed axis in runs, so that blocks fill the card: eight turns a run or more, results within kSumsBytes.
 static int splits_of(int64_t M, int64_t N, int64_t K, int shape, int pairs) {
@@ -311,12 +362,12 @@ static int splits_of(int64_t M, int64_t N, int64_t K, int shape, int pairs) {
 
 struct XentPlan {
   int64_t fwd_piece, piece, ld_dz;
-  int fwd_shape, shape, hidden_shape, hidden_splits, weight_shape, weight_splits;
+  int fwd_shape, fwd_splits, shape, splits, hidden_shape, hidden_splits, weight_shape, weight_splits;
   int64_t parts;
   bool hidden_sums;
   size_t lay_h, lay_w, lay_w_fwd;                        // bytes of laid-out operands
-  size_t part, picked, each, row_sums;                   // forward
-  size_t dz, sums_h, sums_w, row_scale, keep, scalars;   // backward
+  size_t part, picked, each, row_sums, sums_f;           // forward
+  size_t dz, sums_z, sums_h, sums_w, row_scale, keep, scalars;  // backward
 };
 
 static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
@@ -333,24 +384,33 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
     if (most / round * round * count >= classes) return most / round * round;
     return up_to((classes + count - 1) / count, 256);
   };
-  p.fwd_shape = shape_of(classes, rows, 1);
+  const int pairs = P == 1 ? 1 : 6;
+  const int64_t dim_turns = (dim + kDepth - 1) / kDepth * pairs;
+  p.fwd_shape = shape_of(classes, rows, 1, dim_turns);
   p.parts = (classes + kPlans[p.fwd_shape].bm - 1) / kPlans[p.fwd_shape].bm * kPlans[p.fwd_shape].wm;
   p.fwd_piece = pieces(std::min(kPieceMost * 8, kPieceBytes / (ld * 2)));
   p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * 2), dtype == kF32 ? kPieceBytes / (ld * 2) : kPieceMost}));
   p.ld_dz = up_to(p.piece, 8);
-  p.shape = shape_of(p.piece, rows, 1);
+  p.shape = shape_of(p.piece, rows, 1, dim_turns);
+  // logits by split sums: where their tiles leave compute units idle through a long sum
+  const auto split = [&](int64_t M, int shape) { return dim_turns < 16 ? 1 : splits_of(M, rows, dim, shape, pairs); };
+  p.fwd_splits = classes <= p.fwd_piece ? split(classes, p.fwd_shape) : 1;
+  p.splits = split(p.piece, p.shape);
+  if (p.fwd_splits > 1) p.parts = 1;
   const int64_t long_k = std::max<int64_t>(1, p.piece / kDepth / 16), long_n = std::max<int64_t>(1, rows / kDepth / 16);
-  p.hidden_shape = shape_of(dim, rows, long_k);
-  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape, P == 1 ? 1 : 6);
+  p.hidden_shape = shape_of(dim, rows, long_k, p.piece / kDepth * pairs);
+  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape, pairs);
   p.hidden_sums = p.hidden_splits > 1 || p.piece < classes;
-  p.weight_shape = shape_of(dim, p.piece, long_n);
-  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, P == 1 ? 1 : 6);
+  p.weight_shape = shape_of(dim, p.piece, long_n, rows / kDepth * pairs);
+  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, pairs);
   p.lay_h = align256((size_t)rows * ld * 2 * P);
   p.lay_w = align256((size_t)p.piece * ld * 2 * P);
   p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * 2 * P);
   p.part = align256((size_t)rows * p.parts * sizeof(float2));
   p.picked = p.each = align256((size_t)rows * 4);
   p.row_sums = align256(256 * sizeof(RowSum));
+  p.sums_f = p.fwd_splits > 1 ? align256((size_t)p.fwd_splits * rows * classes * 4) : 0;
+  p.sums_z = p.splits > 1 ? align256((size_t)p.splits * rows * p.piece * 4) : 0;
   p.dz = align256((size_t)rows * p.ld_dz * 2 * P);
   p.sums_h = p.hidden_sums ? align256((size_t)p.hidden_splits * rows * dim * 4) : 0;
   p.sums_w = p.weight_splits > 1 ? align256((size_t)p.weight_splits * p.piece * dim * 4) : 0;
@@ -362,8 +422,8 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
 
 size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int dtype, bool backward) {
   const XentPlan p = xent_plan(rows, dim, classes, dtype);
-  if (!backward) return p.lay_h + p.lay_w_fwd + p.part + p.picked + p.each + p.row_sums;
-  return p.lay_h + p.lay_w + p.dz + p.sums_h + p.sums_w + p.row_scale + p.keep + p.scalars;
+  if (!backward) return p.lay_h + p.lay_w_fwd + p.part + p.picked + p.each + p.row_sums + p.sums_f;
+  return p.lay_h + p.lay_w + p.dz + p.sums_z + p.sums_h + p.sums_w + p.row_scale + p.keep + p.scalars;
 }
 
 struct Room {  // hands out a workspace
@@ -401,6 +461,7 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   float* picked = static_cast<float*>(room.take(p.picked));
   float* each = static_cast<float*>(room.take(p.each));
   RowSum* row_sums = static_cast<RowSum*>(room.take(p.row_sums));
+  float* sums = static_cast<float*>(room.take(p.sums_f));
   if (a.reduction == kEach) each = a.loss;
   const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
   ProductArgs g{};
@@ -408,7 +469,8 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   g.b = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), &lh);
   g.N = a.rows;
   g.K = a.dim;
-  g.splits = 1;
+  g.splits = p.fwd_splits;
+  g.sums = sums;
   g.labels = a.labels;
   g.part = part;
   g.parts = p.parts;
@@ -417,7 +479,7 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   const ProductPlan& plan = kPlans[p.fwd_shape];
   // (all classes at once where nothing is laid out, but no more blocks than a grid may have)
   const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 22) / ((a.rows + plan.bn - 1) / plan.bn)) * plan.bm;
-  const int64_t piece = std::min(own ? a.classes : p.fwd_piece, std::max<int64_t>(256, most / 256 * 256));
+  const int64_t piece = p.fwd_splits > 1 ? a.classes : std::min(own ? a.classes : p.fwd_piece, std::max<int64_t>(256, most / 256 * 256));
   hipError_t e = hipSuccess;
   for (int64_t v0 = 0; v0 < a.classes && e == hipSuccess; v0 += piece) {
     const int64_t count = std::min(piece, a.classes - v0);
@@ -427,10 +489,16 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
     g.M = count;
     g.v0 = v0;
     g.part0 = v0 / plan.bm * plan.wm;
-    e = launch_product<E, T>(kLogits, true, p.fwd_shape, g, st);
+    e = launch_product<E, T>(kLogits, p.fwd_splits > 1 ? kSums : kForward, p.fwd_shape, g, st);
   }
   if (e != hipSuccess) return e;
   int team = 64;
+  if (p.fwd_splits > 1) {
+    while (team > 1 && team / 2 >= a.classes) team /= 2;
+    hipLaunchKernelGGL(xent_fold_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, sums, p.fwd_splits,
+                       part, picked, team);
+    team = 64;
+  }
   while (team > 1 && team / 2 >= p.parts) team /= 2;
   if (p.parts <= 512 && a.rows * (p.parts + 8) <= 16384) {
     hipLaunchKernelGGL(xent_short_kernel, dim3(1), dim3(kSumThreads), 0, st, a, part, picked, each, p.parts, team);
@@ -463,7 +531,7 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
   Room room{static_cast<char*>(a.ws)};
   void *lay_h = room.take(p.lay_h), *lay_w = room.take(p.lay_w), *dz = room.take(p.dz);
-  float *sums_h = static_cast<float*>(room.take(p.sums_h)), *sums_w = static_cast<float*>(room.take(p.sums_w));
+  float *sums_z = static_cast<float*>(room.take(p.sums_z)), *sums_h = static_cast<float*>(room.take(p.sums_h)), *sums_w = static_cast<float*>(room.take(p.sums_w));
   float* row_scale = static_cast<float*>(room.take(p.row_scale));
   unsigned long long* keep = static_cast<unsigned long long*>(room.take(p.keep));
   float* scale = static_cast<float*>(room.take(p.scalars));
@@ -485,17 +553,22 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
     ProductArgs g{};
     g.scale = scale;
     // dz of the piece
-    g.a = wm; g.b = hm; g.M = count; g.N = a.rows; g.K = a.dim; g.splits = 1;
+    g.a = wm; g.b = hm; g.M = count; g.N = a.rows; g.K = a.dim; g.splits = p.splits; g.sums = sums_z; g.add = 0;
     g.labels = a.labels; g.ignore = a.ignore; g.v0 = v0; g.stats = a.stats; g.row_scale = row_scale;
     g.dz = dz; g.dz_ld = ld; g.dz_plane = a.rows * ld;
-    if ((e = launch_product<E, T>(kLogits, false, p.shape, g, st)) != hipSuccess) return e;
+    if ((e = launch_product<E, T>(kLogits, p.splits > 1 ? kSums : kBackward, p.shape, g, st)) != hipSuccess) return e;
+    if (p.splits > 1) {
+      const unsigned blocks = (unsigned)std::min<int64_t>((a.rows * ld + 255) / 256, 4096);
+      hipLaunchKernelGGL((xent_dz_kernel<E, sizeof(T) == 4 ? 3 : 1>), dim3(blocks), dim3(256), 0, st, a, sums_z, p.splits, v0, count,
+                         ld, row_scale, static_cast<unsigned short*>(dz));
+    }
     if (a.dh) {
       g.a = wm; g.b = zm; g.M = a.dim; g.N = a.rows; g.K = count;
       g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape, planes_of(dtype) == 1 ? 1 : 6));
       g.sums = p.hidden_sums ? sums_h : nullptr;
       g.add = v0 > 0;
       g.out = a.dh;
-      if ((e = launch_product<E, T>(kHidden, false, p.hidden_shape, g, st)) != hipSuccess) return e;
+      if ((e = launch_product<E, T>(kHidden, 0, p.hidden_shape, g, st)) != hipSuccess) return e;
     }
     if (a.dw) {
       T* out = static_cast<T*>(a.dw) + v0 * a.dim;
@@ -504,7 +577,7 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
       g.sums = p.weight_splits > 1 ? sums_w : nullptr;
       g.add = 0;
       g.out = out;
-      if ((e = launch_product<E, T>(kWeight, false, p.weight_shape, g, st)) != hipSuccess) return e;
+      if ((e = launch_product<E, T>(kWeight, 0, p.weight_shape, g, st)) != hipSuccess) return e;
       if (g.sums) xent_out(sums_w, p.weight_splits, count * a.dim, scale, out, st);
     }
   }

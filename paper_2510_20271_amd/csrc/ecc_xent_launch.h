@@ -25,17 +25,19 @@ static hipError_t product_go(const ProductArgs& g, int threads, hipStream_t st) 
 }
 
 template <typename T, typename O, int BM, int BN, int WM, int WN, int STAGES>
-static hipError_t product_shape(int kind, bool forward, const ProductArgs& g, hipStream_t st) {
+static hipError_t product_shape(int kind, int mode, const ProductArgs& g, hipStream_t st) {
   constexpr int kShared = STAGES * (BM + BN) * kDepth * 2, kThreads = WM * WN * 64;
-  if (kind == kLogits)
-    return forward ? product_go<product_kernel<T, O, kLogits, true, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st)
-                   : product_go<product_kernel<T, O, kLogits, false, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
-  if (kind == kHidden) return product_go<product_kernel<T, O, kHidden, false, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
-  return product_go<product_kernel<T, O, kWeight, false, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kLogits && mode == kForward)
+    return product_go<product_kernel<T, O, kLogits, kForward, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kLogits && mode == kBackward)
+    return product_go<product_kernel<T, O, kLogits, kBackward, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kLogits) return product_go<product_kernel<T, O, kLogits, kSums, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kHidden) return product_go<product_kernel<T, O, kHidden, 0, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  return product_go<product_kernel<T, O, kWeight, 0, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
 }
 
 template <typename T, typename O>
-hipError_t launch_product(int kind, bool forward, int shape, ProductArgs g, hipStream_t st) {
+hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStream_t st) {
   const ProductPlan& p = kPlans[shape];
   g.tiles_m = (int)((g.M + p.bm - 1) / p.bm);
   g.tiles_n = (int)((g.N + p.bn - 1) / p.bn);
@@ -44,15 +46,15 @@ hipError_t launch_product(int kind, bool forward, int shape, ProductArgs g, hipS
   g.splits = (g.total + g.steps - 1) / g.steps;  // (no run is empty)
   const int turns = g.steps * (sizeof(O) == 4 ? 6 : 1);
   switch (shape) {
-    case 0: return product_shape<T, O, 256, 256, 2, 4, 2>(kind, forward, g, st);
-    case 1: return product_shape<T, O, 128, 128, 2, 2, 2>(kind, forward, g, st);
+    case 0: return product_shape<T, O, 256, 256, 2, 4, 2>(kind, mode, g, st);
+    case 1: return product_shape<T, O, 128, 128, 2, 2, 2>(kind, mode, g, st);
     // four tiles in LDS leave room for half the blocks: only where there are tiles to come (one tile of 64 elements, 524288 x 64 x
     // 21 in bfloat16: 20 us with two, 28 with four; six turns or more, 32 x 128 x 1000 in float32: 10.4 with two, 7.8 with four)
-    case 2: return turns < 4 ? product_shape<T, O, 128, 32, 4, 1, 2>(kind, forward, g, st)
-                             : product_shape<T, O, 128, 32, 4, 1, 4>(kind, forward, g, st);
-    case 3: return turns < 4 ? product_shape<T, O, 32, 128, 1, 4, 2>(kind, forward, g, st)
-                             : product_shape<T, O, 32, 128, 1, 4, 4>(kind, forward, g, st);
-    default: return product_shape<T, O, 64, 256, 1, 4, 2>(kind, forward, g, st);
+    case 2: return turns < 4 ? product_shape<T, O, 128, 32, 4, 1, 2>(kind, mode, g, st)
+                             : product_shape<T, O, 128, 32, 4, 1, 4>(kind, mode, g, st);
+    case 3: return turns < 4 ? product_shape<T, O, 32, 128, 1, 4, 2>(kind, mode, g, st)
+                             : product_shape<T, O, 32, 128, 1, 4, 4>(kind, mode, g, st);
+    default: return product_shape<T, O, 64, 256, 1, 4, 2>(kind, mode, g, st);
   }
 }
 

@@ -19,6 +19,8 @@
 namespace ecc {
 
 constexpr int kLogits = 0, kHidden = 1, kWeight = 2;
+// of kLogits: what is made of them; kSums: nothing yet, their sums are split
+constexpr int kBackward = 0, kForward = 1, kSums = 2;
 constexpr int kDepth = 64;  // of a tile along the summed axis
 
 // A matrix of 16-bit elements [planes][rows][ld], ld a multiple of 8, 16-byte aligned; elements between a row's end and ld are 0.
@@ -36,7 +38,7 @@ struct ProductArgs {
   int total;
   const unsigned long long* keep;  // kWeight: bit i of the rows that count (others read as zeros)
   // results
-  float* sums;         // kHidden, kWeight: [splits][N][M], or null: straight to out
+  float* sums;         // kHidden, kWeight, kSums: [splits][N][M], or null: straight to out
   int add;             //   added to what is there
   void* out;           // [N][M], scaled by *scale
   const float* scale;
@@ -217,7 +219,7 @@ __device__ __forceinline__ void wait_and_meet() {
 
 // O: element type of the result;  BM x BN: a block's tile of C, WM x WN waves;  STAGES: tiles in LDS, all but one of them on
 // their way (thin tiles are computed faster than one arrives)
-template <typename T, typename O, int KIND, bool FORWARD, int BM, int BN, int WM, int WN, int STAGES>
+template <typename T, typename O, int KIND, int MODE, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs g) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
@@ -304,30 +306,46 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   for (int j = 0; j < TN; ++j) {
     const int64_t n = n0 + bn + j * 32 + (lane & 31);
     const bool in = n < g.N;
-    if constexpr (KIND == kLogits && FORWARD) {
+    if constexpr (KIND == kLogits && MODE == kForward) {
       const int want = near(in ? g.labels[n] - g.v0 - m0 - am - rows0 : -1), left = near(g.M - m0 - am - rows0);
       float top = -INFINITY, sum = 0.0f, picked = 0.0f;
+      // a wave whose classes are all there and no row's label (almost all, with many classes): no comparisons
+      const bool plain = left >= TM * 32 && __ballot(want >= 0 && want < TM * 32) == 0;
+      if (plain) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int row = i * 32 + 8 * (r / 4) + r % 4;
-          if (row < left) top = fmaxf(top, acc[i][j][r]);
-          picked = row == want ? acc[i][j][r] : picked;
-        }
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int row = i * 32 + 8 * (r / 4) + r % 4;
+            if (row < left) top = fmaxf(top, acc[i][j][r]);
+            picked = row == want ? acc[i][j][r] : picked;
+          }
+      }
       top = fmaxf(top, __shfl_xor(top, 32));
       const float base = top == -INFINITY ? 0.0f : top;
+      if (plain) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int row = i * 32 + 8 * (r / 4) + r % 4;
-          if (row < left && row != want) sum += __expf(acc[i][j][r] - base);
-        }
+          for (int r = 0; r < 16; ++r) sum += __expf(acc[i][j][r] - base);
+      } else {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int row = i * 32 + 8 * (r / 4) + r % 4;
+            if (row < left && row != want) sum += __expf(acc[i][j][r] - base);
+          }
+      }
       sum += __shfl_xor(sum, 32);
       if (want >= 0 && want < min(left, TM * 32) && !(want & 4)) g.picked[n] = picked;  // (a lane has rows 0 .. 3 of every 8)
       if (in && lane < 32) g.part[n * g.parts + g.part0 + (int64_t)tm * WM + wave % WM] = make_float2(top, sum);
-    } else if constexpr (KIND == kLogits) {
+    } else if constexpr (KIND == kLogits && MODE == kBackward) {
       const int64_t label = in ? g.labels[n] : -1;
       const int want = near(label - g.v0 - m0 - am - rows0), left = near(g.M - m0 - am - rows0);
       const bool counts = in && label != g.ignore;
@@ -419,6 +437,6 @@ constexpr ProductPlan kPlans[] = {{256, 256, 2}, {128, 128, 2}, {128, 32, 4}, {3
 
 // g.a .. g.K, splits set; tiles, steps and total are filled in here
 template <typename T, typename O>
-hipError_t launch_product(int kind, bool forward, int shape, ProductArgs g, hipStream_t st);
+hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStream_t st);
 
 }  // namespace ecc
