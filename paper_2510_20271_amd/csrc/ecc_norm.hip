@@ -820,7 +820,7 @@ static int norm_vector(const NormArgs& a, int size) {
 
 // Rows of a block.  What a block does beside its rows -- scales, the joining of its sums -- is as much as some ten rows, so
 // threads take 16 of them; fewer (four at the least) where 16 would leave compute units without a block.  (2 x 83193 x 44 in
-// float32 with four rows a thread: sums 28.7 us, second sweep 20.0; a thread takes NORM_AFTER.)
+// float32 with four rows a thread: sums 28.7 us, second sweep 20.0; with sixteen 14.0 and 15.2.)
 static void share_rows(NormGeo& g, int64_t items) {
   g.lanes = (int)std::max<int64_t>(1, std::min<int64_t>(kNormThreads / g.wide, g.rows));
   const auto parts_of = [&](int64_t each) { return std::max<int64_t>(1, (g.rows + g.lanes * each - 1) / (g.lanes * each)); };

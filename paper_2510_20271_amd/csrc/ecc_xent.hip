@@ -341,7 +341,7 @@ static int ld_of(int dim) { return (int)up_to(dim, 8); }
 
 // Tiles of 256 x 256 where they fill the card (one block a CU) and the summed axis is eight turns or more; of 128 x 128
 // otherwise, two blocks a CU, so that one's start and end run beside the other's products.  Thin products have thin tiles.
-// (385475 x 18 x 599 in float16, one turn: logits 228 us by large tiles, XENT_AFTER by the others.)
+// (385475 x 18 x 599 in float16, one turn: logits 228 us by large tiles, 176 by the others.)
 static int shape_of(int64_t M, int64_t N, int64_t runs, int64_t turns) {
   if (N <= 32) return 2;
   if (M <= 32) return 3;
@@ -393,7 +393,10 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   p.ld_dz = up_to(p.piece, 8);
   p.shape = shape_of(p.piece, rows, 1, dim_turns);
   // logits by split sums: where their tiles leave compute units idle through a long sum
-  const auto split = [&](int64_t M, int shape) { return dim_turns < 16 ? 1 : splits_of(M, rows, dim, shape, pairs); };
+  const auto split = [&](int64_t M, int shape) {
+    const int splits = dim_turns < 16 || M > 4096 ? 1 : splits_of(M, rows, dim, shape, pairs);
+    return splits >= 4 ? splits : 1;
+  };
   p.fwd_splits = classes <= p.fwd_piece ? split(classes, p.fwd_shape) : 1;
   p.splits = split(p.piece, p.shape);
   if (p.fwd_splits > 1) p.parts = 1;
@@ -507,6 +510,8 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   if (a.rows < 512 && p.parts > 512) {
     hipLaunchKernelGGL(xent_long_row_kernel, dim3((unsigned)a.rows), dim3(1024), 0, st, a, part, picked, each, p.parts);
   } else {
+    // (one lane of a team ends its row, in float64: no larger teams than fill the card)
+    while (team > 1 && a.rows * (team / 2) >= 131072 && p.parts <= 4 * team) team /= 2;
     hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, part, picked, each,
                        p.parts, team);
   }

@@ -45,16 +45,21 @@ hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStrea
   g.steps = (g.total + g.splits - 1) / g.splits;
   g.splits = (g.total + g.steps - 1) / g.steps;  // (no run is empty)
   const int turns = g.steps * (sizeof(O) == 4 ? 6 : 1);
+  // One turn needs one tile in LDS, which leaves room for more blocks (385475 x 18 x 599 in float16: logits 176 us with two,
+  // 145 with one); thin tiles are four ahead where there are turns to come (32 x 128 x 1000 in float32: 10.4 us with two,
+  // 7.8 with four).
   switch (shape) {
     case 0: return product_shape<T, O, 256, 256, 2, 4, 2>(kind, mode, g, st);
-    case 1: return product_shape<T, O, 128, 128, 2, 2, 2>(kind, mode, g, st);
-    // four tiles in LDS leave room for half the blocks: only where there are tiles to come (one tile of 64 elements, 524288 x 64 x
-    // 21 in bfloat16: 20 us with two, 28 with four; six turns or more, 32 x 128 x 1000 in float32: 10.4 with two, 7.8 with four)
-    case 2: return turns < 4 ? product_shape<T, O, 128, 32, 4, 1, 2>(kind, mode, g, st)
-                             : product_shape<T, O, 128, 32, 4, 1, 4>(kind, mode, g, st);
-    case 3: return turns < 4 ? product_shape<T, O, 32, 128, 1, 4, 2>(kind, mode, g, st)
-                             : product_shape<T, O, 32, 128, 1, 4, 4>(kind, mode, g, st);
-    default: return product_shape<T, O, 64, 256, 1, 4, 2>(kind, mode, g, st);
+    case 1: return turns == 1 ? product_shape<T, O, 128, 128, 2, 2, 1>(kind, mode, g, st)
+                              : product_shape<T, O, 128, 128, 2, 2, 2>(kind, mode, g, st);
+    case 2: return turns == 1  ? product_shape<T, O, 128, 32, 4, 1, 1>(kind, mode, g, st)
+                   : turns < 4 ? product_shape<T, O, 128, 32, 4, 1, 2>(kind, mode, g, st)
+                               : product_shape<T, O, 128, 32, 4, 1, 4>(kind, mode, g, st);
+    case 3: return turns == 1  ? product_shape<T, O, 32, 128, 1, 4, 1>(kind, mode, g, st)
+                   : turns < 4 ? product_shape<T, O, 32, 128, 1, 4, 2>(kind, mode, g, st)
+                               : product_shape<T, O, 32, 128, 1, 4, 4>(kind, mode, g, st);
+    default: return turns == 1 ? product_shape<T, O, 64, 256, 1, 4, 1>(kind, mode, g, st)
+                               : product_shape<T, O, 64, 256, 1, 4, 2>(kind, mode, g, st);
   }
 }
 

@@ -208,6 +208,55 @@ __device__ __forceinline__ void tile_of(int block, int blocks, int tiles_m, int 
   m = band * 4 + in - n * high;
 }
 
+// A wave's results on their way to memory: 32 columns of C (rows of the result) of TM x 32 elements, turned in the wave's part of
+// LDS so that stores run along the result's rows.  Chunk c of row n at c ^ n: writes and reads are spread over the banks.
+template <typename E, int TM>
+struct Turn {
+  static constexpr int kRow = TM * 32 * sizeof(E), kChunks = kRow / 16, kBytes = 32 * kRow, kPer = 16 / sizeof(E);
+  __device__ __forceinline__ static unsigned char* place(unsigned char* room, int n, int c) {
+    return room + n * kRow + ((c ^ (n & (kChunks - 1))) << 4);
+  }
+  // four elements from column m (a multiple of 4) of row n
+  __device__ __forceinline__ static void put(unsigned char* room, int n, int m, const E (&e)[4]) {
+    unsigned char* at = place(room, n, m * (int)sizeof(E) / 16) + m * (int)sizeof(E) % 16;
+    if constexpr (sizeof(E) == 4) {
+      uint4 w;
+      __builtin_memcpy(&w, e, 16);
+      *reinterpret_cast<uint4*>(at) = w;
+    } else {
+      uint2 w;
+      __builtin_memcpy(&w, e, 8);
+      *reinterpret_cast<uint2*>(at) = w;
+    }
+  }
+  // rows and columns that are there; out: element (0, 0), rows `ld` apart.  step: bytes that every row and `out` are multiples of
+  __device__ __forceinline__ static void store(unsigned char* room, int lane, E* out, int64_t ld, int64_t rows, int64_t columns,
+                                               int step) {
+#pragma unroll
+    for (int k = 0; k < kChunks / 2; ++k) {
+      const int at = k * 64 + lane, n = at / kChunks, c = at % kChunks;
+      const uint4 w = *reinterpret_cast<const uint4*>(place(room, n, c));
+      const int64_t left = columns - c * kPer;
+      if (n >= rows || left <= 0) continue;
+      E* to = out + n * ld + c * kPer;
+      if (step >= 16) {
+        *reinterpret_cast<uint4*>(to) = w;
+      } else if (step >= 4) {
+        const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i * 4 < left * (int)sizeof(E)) reinterpret_cast<unsigned*>(to)[i] = u[i];
+      } else {
+        E e[kPer];
+        __builtin_memcpy(e, &w, 16);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (i < left) to[i] = e[i];
+      }
+    }
+  }
+};
+
 // a distance between classes as far as a tile is concerned
 __device__ __forceinline__ int near(int64_t d) { return (int)(d < -1 ? -1 : d > 1024 ? 1024 : d); }
 
@@ -264,10 +313,11 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
     }
   };
   const int am = (wave % WM) * (BM / WM), bn = (wave / WM) * (BN / WN);
+  // (STAGES 1: for one turn)
 #pragma unroll
-  for (int t = 0; t < STAGES - 1; ++t) fetch(t);
+  for (int t = 0; t < (STAGES > 1 ? STAGES - 1 : 1); ++t) fetch(t);
   for (int t = 0; t < turns; ++t) {
-    wait_and_meet<(STAGES - 2) * (TA::kEach + TB::kEach)>();  // the tile is there, and the one before has been read
+    wait_and_meet<STAGES < 3 ? 0 : (STAGES - 2) * (TA::kEach + TB::kEach)>();  // the tile is there, and the one before has been read
     const unsigned char* from = smem + t % STAGES * kBoth;
     typename TA::V8 a[2][TM], b[2][TN];
     const auto read = [&](int ks) {
@@ -285,9 +335,9 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mma(a[ks & 1][i], b[ks & 1][j], acc[i][j]);
       interleave<TM * TN, TA::kReads * TM + TB::kReads * TN>();
-      if (ks == 0) fetch(t + STAGES - 1);
+      if (STAGES > 1 && ks == 0) fetch(t + STAGES - 1);
     }
-    if (kTwoSums && t % 8 == 7) {
+    if (kTwoSums && STAGES > 1 && t % 8 == 7) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         total[r] += acc[0][0][r];
@@ -295,11 +345,11 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
       }
     }
   }
-  if (kTwoSums) {
+  if (kTwoSums && STAGES > 1) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[0][0][r] += total[r];
   }
-  wait_and_meet<0>();  // (the last fetches have to land before the block's LDS is another's)
+  wait_and_meet<0>();  // the last fetches have landed and the tiles are read: LDS is free
 
   const int rows0 = 4 * (lane >> 5);  // accumulator r is row 8 (r / 4) + rows0 + r % 4 of its 32
 #pragma unroll
@@ -354,51 +404,48 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int64_t v = m0 + am + i * 32 + 8 * q + rows0;  // four classes from here
-          float f[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int row = i * 32 + 8 * q + r;
-            const float p = row == want ? -miss : __expf((acc[i][j][q * 4 + r] - lse) - rest);
-            f[r] = counts && row < left ? p * scale : 0.0f;
-          }
-          if (!in || v >= g.dz_ld) continue;  // (dz_ld is a multiple of 8)
-          unsigned short* to = static_cast<unsigned short*>(g.dz) + n * g.dz_ld + v;
-          if constexpr (kPairs == 1) {
-            T h[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) h[r] = narrow<T>(f[r]);
-            uint2 w;
-            __builtin_memcpy(&w, h, 8);
-            *reinterpret_cast<uint2*>(to) = w;
-          } else {
-            unsigned short s[4][3];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) split3(f[r], s[r]);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-              const uint2 w = make_uint2((unsigned)s[0][k] | (unsigned)s[1][k] << 16, (unsigned)s[2][k] | (unsigned)s[3][k] << 16);
-              *reinterpret_cast<uint2*>(to + k * g.dz_plane) = w;
-            }
-          }
+        for (int r = 0; r < 16; ++r) {
+          const int row = i * 32 + 8 * (r / 4) + r % 4;
+          const float p = row == want ? -miss : __expf((acc[i][j][r] - lse) - rest);
+          acc[i][j][r] = counts && row < left ? p * scale : 0.0f;
         }
+      using Out = Turn<unsigned short, TM>;
+      unsigned char* room = smem + wave * Out::kBytes;
+#pragma unroll
+      for (int k = 0; k < (kPairs == 1 ? 1 : 3); ++k) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            unsigned short e[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              if constexpr (kPairs == 1) {
+                e[r] = __builtin_bit_cast(unsigned short, narrow<T>(acc[i][j][q * 4 + r]));
+              } else {  // the leading 8 bits, and what is left for the next plane
+                const unsigned bits = __float_as_uint(acc[i][j][q * 4 + r]);
+                e[r] = (unsigned short)(bits >> 16);
+                acc[i][j][q * 4 + r] -= __uint_as_float(bits & 0xffff0000u);
+              }
+            }
+            Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);
+          }
+        const int64_t first = n0 + bn + j * 32;
+        Out::store(room, lane, static_cast<unsigned short*>(g.dz) + k * g.dz_plane + first * g.dz_ld + m0 + am, g.dz_ld,
+                   g.N - first, g.dz_ld - m0 - am, 16);
+      }
     } else {
-      const float scale = g.sums ? 1.0f : *g.scale;
+      if (g.sums) {
+        const bool four = g.M % 4 == 0;
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int64_t m = m0 + am + i * 32 + 8 * q + rows0;
-          if (!in || m >= g.M) continue;
-          float f[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) f[r] = acc[i][j][q * 4 + r];
-          const bool four = g.M % 4 == 0;
-          if (g.sums) {
+          for (int q = 0; q < 4; ++q) {
+            const int64_t m = m0 + am + i * 32 + 8 * q + rows0;
+            if (!in || m >= g.M) continue;
             float* to = g.sums + ((int64_t)split * g.N + n) * g.M + m;
             if (four) {
-              float4 w = make_float4(f[0], f[1], f[2], f[3]);
+              float4 w = make_float4(acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]);
               if (g.add) {
                 const float4 o = *reinterpret_cast<const float4*>(to);
                 w.x += o.x; w.y += o.y; w.z += o.z; w.w += o.w;
@@ -407,25 +454,27 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
             } else {
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                if (m + r < g.M) to[r] = g.add ? to[r] + f[r] : f[r];
-            }
-          } else {
-            O* to = static_cast<O*>(g.out) + n * g.M + m;
-            O h[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) h[r] = narrow<O>(f[r] * scale);
-            if (four && (reinterpret_cast<uintptr_t>(g.out) & (sizeof(O) * 4 - 1)) == 0) {
-              struct alignas(sizeof(O) * 4) Four { O e[4]; } w;
-#pragma unroll
-              for (int r = 0; r < 4; ++r) w.e[r] = h[r];
-              *reinterpret_cast<Four*>(to) = w;
-            } else {
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (m + r < g.M) to[r] = h[r];
+                if (m + r < g.M) to[r] = g.add ? to[r] + acc[i][j][q * 4 + r] : acc[i][j][q * 4 + r];
             }
           }
-        }
+      } else {
+        using Out = Turn<O, TM>;
+        unsigned char* room = smem + wave * Out::kBytes;
+        const float scale = *g.scale;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            O e[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) e[r] = narrow<O>(acc[i][j][q * 4 + r] * scale);
+            Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);
+          }
+        const int64_t first = n0 + bn + j * 32;
+        const unsigned low = (unsigned)(uintptr_t)g.out | (unsigned)(g.M * sizeof(O));
+        Out::store(room, lane, static_cast<O*>(g.out) + first * g.M + m0 + am, g.M, g.N - first, g.M - m0 - am,
+                   low % 16 == 0 ? 16 : low % 4 == 0 ? 4 : 2);
+      }
     }
   }
 }

@@ -230,3 +230,44 @@ def test_refusals():
         with pytest.raises(api.EccError) as e:
             call()
         assert e.value.status == status
+
+
+def test_features_beyond_32_bits():
+    """2.15e9 features in one item: statistics over all of them, the last points' outputs and gradients."""
+    S, C, G = (1 << 25) + 5, 64, 8
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    x = torch.empty(1, S, C, dtype=BF16, device="cuda").normal_(generator=gen)
+    dy = torch.empty(1, S, C, dtype=BF16, device="cuda").normal_(generator=gen)
+    w = 1 + 0.3 * torch.randn(C, generator=gen, device="cuda")
+    b = 0.3 * torch.randn(C, generator=gen, device="cuda")
+    y, stats = api.ecc_norm_fwd(x, G, w, b)
+    gx, gw, gb = api.ecc_norm_bwd(x, dy, G, stats, w, b)
+    part, m = 1 << 21, S * (C // G)
+
+    def over(f):
+        total = 0.0
+        for r in range(0, S, part):
+            total = total + f(x[0, r:r + part].double(), dy[0, r:r + part].double())
+        return total
+
+    def spread(t):
+        return t.repeat_interleave(C // G)
+    mean = over(lambda a, d: a.sum(0)).view(G, -1).sum(1) / m
+    rstd = 1 / torch.sqrt(over(lambda a, d: ((a - spread(mean)) ** 2).sum(0)).view(G, -1).sum(1) / m + 1e-5)
+    assert float((stats[0, :, 0] - mean).abs().max()) < 1e-6 and float((stats[0, :, 1] / rstd - 1).abs().max()) < 1e-6
+
+    def terms(a, d):
+        xhat = (a - spread(mean)) * spread(rstd)
+        v = xhat * w + b
+        s = torch.sigmoid(v)
+        return xhat, v * s, d * s * (1 + v * (1 - s))
+    db = over(lambda a, d: terms(a, d)[2].sum(0))
+    dw = over(lambda a, d: (terms(a, d)[2] * terms(a, d)[0]).sum(0))
+    # 2^31 / 64 terms of size 1 with random signs: sums of about 6e3, off by 300 E of the 3e7 terms' sizes at most
+    assert float((gb - db).abs().max()) < 300 * E * S and float((gw - dw).abs().max()) < 300 * E * S
+    xhat, want, dv = terms(x[0, -100:].double(), dy[0, -100:].double())
+    assert bool(((y[0, -100:].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all())
+    m1 = spread((db * w).view(G, -1).sum(1) / m)
+    m2 = spread((dw * w).view(G, -1).sum(1) / m)
+    want = spread(rstd) * (dv * w - m1 - xhat * m2)
+    assert bool(((gx[0, -100:].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all())

@@ -274,3 +274,69 @@ def test_large_tiles(dtype):
     """Enough rows, classes and features for the largest tiles of all three products, ragged in each."""
     h, W, labels, up = _data(2300, 1032 if dtype == BF16 else 520, 9001, dtype, seed=12)
     _check(h, W, labels, "mean", up)
+
+
+@pytest.mark.parametrize("n,d,V,dtype", [(4100, 16, 40000, BF16), (4100, 16, 33000, F16), (4100, 9, 33000, F32),
+                                         (3, 4096, 20001, F32), (3, 4095, 20001, BF16)])
+def test_several_pieces(n, d, V, dtype):
+    """More classes than a piece of the logits' gradient, or of laid-out weights, holds."""
+    h, W, labels, up = _data(n, d, V, dtype, seed=13)
+    _check(h, W, labels, "none", up)
+
+
+def test_weights_beyond_32_bits():
+    """2.4e9 weights: the last classes' logits, gradients and what is written for them."""
+    V, d = 590000, 4096
+    gen = torch.Generator(device="cuda").manual_seed(14)
+    W = torch.empty(V, d, dtype=BF16, device="cuda").normal_(generator=gen).mul_(d ** -0.5)
+    h = torch.randn(3, d, generator=gen, device="cuda").to(BF16)
+    labels = torch.tensor([V - 1, 5, V - 2], device="cuda")
+    loss, stats, counted = api.ecc_xent_fwd(h, W, labels, reduction="none")
+    z = torch.cat([h.double() @ W[v:v + 50000].double().t() for v in range(0, V, 50000)], 1)
+    lse = torch.logsumexp(z, 1)
+    want = lse - z[torch.arange(3, device="cuda"), labels]
+    assert float((loss.double() - want).abs().max()) < 1e-4
+    up = torch.ones(3, device="cuda")
+    dh, dW = api.ecc_xent_bwd(h, W, labels, up, stats, counted, reduction="none")
+    p = torch.exp(z - lse[:, None])
+    p[torch.arange(3, device="cuda"), labels] -= 1.0
+    for rows in (slice(0, 64), slice(V - 64, V), slice(524200, 524400)):
+        ref = p[:, rows].t() @ h.double()
+        # held in bfloat16 between the products (2^-9 each), rounded once more at the end
+        assert bool(((dW[rows].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -8 * (p[:, rows].abs().t() @ h.double().abs())).all())
+    ref = torch.zeros(3, d, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(ref)
+    for v in range(0, V, 50000):
+        w = W[v:v + 50000].double()
+        ref += p[:, v:v + 50000] @ w
+        size += p[:, v:v + 50000].abs() @ w.abs()
+    assert bool(((dh.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -8 * size).all())
+
+
+def test_features_beyond_32_bits():
+    """2.15e9 features: the last rows' losses and gradients."""
+    n, d, V = (1 << 25) + 70, 64, 5
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    h = torch.empty(n, d, dtype=BF16, device="cuda").normal_(generator=gen)
+    W = torch.randn(V, d, generator=gen, device="cuda").to(BF16)
+    labels = torch.randint(0, V, (n,), generator=gen, device="cuda")
+    labels[-3] = -100
+    loss, stats, counted = api.ecc_xent_fwd(h, W, labels, reduction="none")
+    assert int(counted) == n - 1
+    up = torch.ones(n, device="cuda")
+    dh, dW = api.ecc_xent_bwd(h, W, labels, up, stats, counted, reduction="none")
+    tail = slice(n - 200, n)
+    ref = xent_reference(h[tail], W, labels[tail], -100, "none", up[tail])
+    within(loss[tail], ref[0], ref[1], "loss")
+    within(dh[tail], ref[2], ref[3], "dhidden")
+    want, size = torch.zeros(V, d, dtype=torch.float64, device="cuda"), torch.zeros(V, d, dtype=torch.float64, device="cuda")
+    part = 1 << 21
+    for r in range(0, n, part):
+        hd, lab = h[r:r + part].double(), labels[r:r + part]
+        p = torch.softmax(hd @ W.double().t(), 1)
+        p[torch.arange(len(lab), device="cuda"), lab.clamp_min(0)] -= 1.0
+        p[lab < 0] = 0.0
+        want += p.t() @ hd
+        size += p.abs().t() @ hd.abs()
+    # dz rounded to bfloat16 (2^-9, independent over 3e7 rows: 4 / sqrt(n) of the sizes' sum) and float32 sums in runs
+    assert bool(((dW.double() - want).abs() <= 2.0 ** -8 * want.abs() + size * (4 * 2.0 ** -9 / n ** 0.5 + 1e-5)).all())
