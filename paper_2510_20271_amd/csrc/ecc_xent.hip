@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <numeric>
+#include <type_traits>
 
 #include "ecc_xent_product.h"
 
@@ -26,30 +27,35 @@ static int64_t up_to(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 // caller's own memory will do.
 struct Lay {
   const void* from;
-  unsigned short* to;
+  void* to;
   int64_t rows, blocks;
 };
-template <typename T>
+template <typename T, bool SPLIT>
 __device__ __forceinline__ void lay_chunk(const Lay& l, int dim, int ld, int64_t block) {
   const T* from = static_cast<const T*>(l.from);
   const int64_t at = (block * 256 + threadIdx.x) * 8, all = l.rows * ld;
   if (at >= all) return;
   const int64_t row = at / ld;
   const int k = (int)(at - row * ld);
-  unsigned short s[8][3];
+  if constexpr (SPLIT) {
+    unsigned short s[8][3];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (sizeof(T) == 4) split3(k + i < dim ? widen(from[row * dim + k + i]) : 0.0f, s[i]);
-    else s[i][0] = k + i < dim ? reinterpret_cast<const unsigned short*>(from)[row * dim + k + i] : 0;
-  }
+    for (int i = 0; i < 8; ++i) split3(k + i < dim ? widen(from[row * dim + k + i]) : 0.0f, s[i]);
 #pragma unroll
-  for (int p = 0; p < (sizeof(T) == 4 ? 3 : 1); ++p) {
-    uint4 w;
-    w.x = (unsigned)s[0][p] | (unsigned)s[1][p] << 16;
-    w.y = (unsigned)s[2][p] | (unsigned)s[3][p] << 16;
-    w.z = (unsigned)s[4][p] | (unsigned)s[5][p] << 16;
-    w.w = (unsigned)s[6][p] | (unsigned)s[7][p] << 16;
-    *reinterpret_cast<uint4*>(l.to + p * all + at) = w;
+    for (int p = 0; p < 3; ++p) {
+      uint4 w;
+      w.x = (unsigned)s[0][p] | (unsigned)s[1][p] << 16;
+      w.y = (unsigned)s[2][p] | (unsigned)s[3][p] << 16;
+      w.z = (unsigned)s[4][p] | (unsigned)s[5][p] << 16;
+      w.w = (unsigned)s[6][p] | (unsigned)s[7][p] << 16;
+      *reinterpret_cast<uint4*>(static_cast<unsigned short*>(l.to) + p * all + at) = w;
+    }
+  } else {
+    using Bits = typename std::conditional<sizeof(T) == 4, unsigned, unsigned short>::type;
+    struct alignas(16) Eight { Bits e[8]; } w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w.e[i] = k + i < dim ? reinterpret_cast<const Bits*>(from)[row * dim + k + i] : (Bits)0;
+    *reinterpret_cast<Eight*>(static_cast<Bits*>(l.to) + at) = w;
   }
 }
 
@@ -133,7 +139,7 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(XentArgs a, const float*
 // ... or their gradient, [planes][rows][ld], for `count` classes from v0
 template <typename E, int PLANES>
 __global__ __launch_bounds__(256) void xent_dz_kernel(XentArgs a, const float* sums, int splits, int64_t v0, int64_t count, int64_t ld,
-                                                      const float* row_scale, unsigned short* dz) {
+                                                      const float* row_scale, E* dz) {
   const int64_t all = a.rows * ld, n = a.rows * count;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / ld, v = i - row * ld, label = a.labels[row];
@@ -145,13 +151,16 @@ __global__ __launch_bounds__(256) void xent_dz_kernel(XentArgs a, const float* s
       const float high = (float)lse, low = (float)(lse - (double)high);
       f = (v0 + v == label ? -(float)a.stats[row * 2 + 1] : __expf((x - high) - low)) * row_scale[row];
     }
-    if constexpr (PLANES == 1) {
-      dz[i] = __builtin_bit_cast(unsigned short, narrow<E>(f));
-    } else {
-      unsigned short p[3];
-      split3(f, p);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) dz[k * all + i] = p[k];
+    for (int k = 0; k < PLANES; ++k) {
+      if constexpr (PLANES == 3) {
+        const unsigned bits = __float_as_uint(f);
+        dz[k * all + i] = __builtin_bit_cast(E, (unsigned short)(bits >> 16));
+        f -= __uint_as_float(bits & 0xffff0000u);
+      } else {
+        dz[k * all + i] = narrow<E>(f);
+        f -= widen(narrow<E>(f));
+      }
     }
   }
 }
@@ -295,12 +304,12 @@ __device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, i
 }
 
 // What comes before the products, in one launch: both operands laid out and the rows' scales, a run of blocks each.
-template <typename T>
+template <typename T, bool SPLIT>
 __global__ __launch_bounds__(256) void xent_prepare_kernel(XentArgs a, Lay h, Lay w, int ld, Scales c) {
   int64_t block = blockIdx.x;
-  if (block < h.blocks) return lay_chunk<T>(h, a.dim, ld, block);
+  if (block < h.blocks) return lay_chunk<T, SPLIT>(h, a.dim, ld, block);
   block -= h.blocks;
-  if (block < w.blocks) return lay_chunk<T>(w, a.dim, ld, block);
+  if (block < w.blocks) return lay_chunk<T, SPLIT>(w, a.dim, ld, block);
   scale_rows(a, c, block - w.blocks);
 }
 
@@ -336,23 +345,30 @@ constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of a plane of dz, and of
 constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
 constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 
-static int planes_of(int dtype) { return dtype == kF32 ? 3 : 1; }
+// float32: by the float32 instruction where rows are few and the weights' way from memory counts (41 x 2363 x 31381: step XENT_PLANES us
+// by planes, XENT_NATIVE so), by planes of bfloat16 otherwise.  16-bit: two planes of dz where rows are few.
+constexpr int64_t kFewRows = 96, kFewHalves = 64;
+static bool native(int64_t rows, int dtype) { return dtype == kF32 && rows <= kFewRows; }
+static int operand_planes(int64_t rows, int dtype) { return dtype == kF32 && !native(rows, dtype) ? 3 : 1; }
+static int gradient_planes(int64_t rows, int dtype) {
+  return dtype == kF32 ? operand_planes(rows, dtype) : rows <= kFewHalves ? 2 : 1;
+}
 static int ld_of(int dim) { return (int)up_to(dim, 8); }
 
 // Tiles of 256 x 256 where they fill the card (one block a CU) and the summed axis is eight turns or more; of 128 x 128
 // otherwise, two blocks a CU, so that one's start and end run beside the other's products.  Thin products have thin tiles.
 // (385475 x 18 x 599 in float16, one turn: logits 228 us by large tiles, 176 by the others.)
-static int shape_of(int64_t M, int64_t N, int64_t runs, int64_t turns) {
+static int shape_of(int64_t M, int64_t N, int64_t runs, int64_t turns, bool few = false) {
   if (N <= 32) return 2;
   if (M <= 32) return 3;
   if (M <= 64 && N > 128) return 4;
   const int64_t large = (M + 255) / 256 * ((N + 255) / 256);
-  return M > 128 && N > 128 && turns >= 8 && large * runs >= 256 ? 0 : 1;
+  return !few && M > 128 && N > 128 && turns >= 8 && large * runs >= 256 ? 0 : 1;
 }
 // The summed axis in runs, so that blocks fill the card: eight turns a run or more, results within kSumsBytes.
-static int splits_of(int64_t M, int64_t N, int64_t K, int shape, int pairs) {
+static int splits_of(int64_t M, int64_t N, int64_t K, int shape, int pairs, int depth) {
   const ProductPlan& p = kPlans[shape];
-  const int64_t blocks = (M + p.bm - 1) / p.bm * ((N + p.bn - 1) / p.bn), total = (K + kDepth - 1) / kDepth;
+  const int64_t blocks = (M + p.bm - 1) / p.bm * ((N + p.bn - 1) / p.bn), total = (K + depth - 1) / depth;
   const int64_t fill = shape == 0 ? 256 : 512;  // blocks that the card holds
   int64_t want = std::min(std::max<int64_t>(1, fill / blocks), std::max<int64_t>(1, total * pairs / 8));
   want = std::max<int64_t>(1, std::min({want, total, kSumsBytes / (M * N * 4)}));
@@ -372,7 +388,9 @@ struct XentPlan {
 
 static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   XentPlan p{};
-  const int P = planes_of(dtype);
+  const int P = operand_planes(rows, dtype), Z = gradient_planes(rows, dtype);
+  const int64_t size = native(rows, dtype) ? 4 : 2;  // of a plane's element
+  const bool few = native(rows, dtype) || Z == 2;
   const int64_t ld = ld_of(dim);
   // Pieces of at most `most` classes, equal ones.  Where the last piece is small anyway the others hold whole rounds of 256 large
   // tiles (2048 rows, 50021 classes: 32768 and 17253, 4 + 3 rounds of blocks; halves: 4 + 4).
@@ -384,37 +402,37 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
     if (most / round * round * count >= classes) return most / round * round;
     return up_to((classes + count - 1) / count, 256);
   };
-  const int pairs = P == 1 ? 1 : 6;
-  const int64_t dim_turns = (dim + kDepth - 1) / kDepth * pairs;
-  p.fwd_shape = shape_of(classes, rows, 1, dim_turns);
+  const int pairs = P == 1 ? 1 : 6, pairs_z = P == 3 ? 6 : Z, depth = 128 / (int)size;
+  const int64_t dim_turns = (dim + depth - 1) / depth * pairs;
+  p.fwd_shape = shape_of(classes, rows, 1, dim_turns, few);
   p.parts = (classes + kPlans[p.fwd_shape].bm - 1) / kPlans[p.fwd_shape].bm * kPlans[p.fwd_shape].wm;
-  p.fwd_piece = pieces(std::min(kPieceMost * 8, kPieceBytes / (ld * 2)));
-  p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * 2), dtype == kF32 ? kPieceBytes / (ld * 2) : kPieceMost}));
+  p.fwd_piece = pieces(std::min(kPieceMost * 8, kPieceBytes / (ld * size)));
+  p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * size), P == 3 ? kPieceBytes / (ld * size) : kPieceMost}));
   p.ld_dz = up_to(p.piece, 8);
-  p.shape = shape_of(p.piece, rows, 1, dim_turns);
+  p.shape = shape_of(p.piece, rows, 1, dim_turns, few);
   // logits by split sums: where their tiles leave compute units idle through a long sum
   const auto split = [&](int64_t M, int shape) {
-    const int splits = dim_turns < 16 || M > 4096 ? 1 : splits_of(M, rows, dim, shape, pairs);
+    const int splits = dim_turns < 16 || M > 4096 ? 1 : splits_of(M, rows, dim, shape, pairs, depth);
     return splits >= 4 ? splits : 1;
   };
   p.fwd_splits = classes <= p.fwd_piece ? split(classes, p.fwd_shape) : 1;
   p.splits = split(p.piece, p.shape);
   if (p.fwd_splits > 1) p.parts = 1;
-  const int64_t long_k = std::max<int64_t>(1, p.piece / kDepth / 16), long_n = std::max<int64_t>(1, rows / kDepth / 16);
-  p.hidden_shape = shape_of(dim, rows, long_k, p.piece / kDepth * pairs);
-  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape, pairs);
+  const int64_t long_k = std::max<int64_t>(1, p.piece / depth / 16), long_n = std::max<int64_t>(1, rows / depth / 16);
+  p.hidden_shape = shape_of(dim, rows, long_k, p.piece / depth * pairs_z, few);
+  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape, pairs_z, depth);
   p.hidden_sums = p.hidden_splits > 1 || p.piece < classes;
-  p.weight_shape = shape_of(dim, p.piece, long_n, rows / kDepth * pairs);
-  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, pairs);
-  p.lay_h = align256((size_t)rows * ld * 2 * P);
-  p.lay_w = align256((size_t)p.piece * ld * 2 * P);
-  p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * 2 * P);
+  p.weight_shape = shape_of(dim, p.piece, long_n, rows / depth * pairs_z, few);
+  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, pairs_z, depth);
+  p.lay_h = align256((size_t)rows * ld * size * P);
+  p.lay_w = align256((size_t)p.piece * ld * size * P);
+  p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * size * P);
   p.part = align256((size_t)rows * p.parts * sizeof(float2));
   p.picked = p.each = align256((size_t)rows * 4);
   p.row_sums = align256(256 * sizeof(RowSum));
   p.sums_f = p.fwd_splits > 1 ? align256((size_t)p.fwd_splits * rows * classes * 4) : 0;
   p.sums_z = p.splits > 1 ? align256((size_t)p.splits * rows * p.piece * 4) : 0;
-  p.dz = align256((size_t)rows * p.ld_dz * 2 * P);
+  p.dz = align256((size_t)rows * p.ld_dz * size * Z);
   p.sums_h = p.hidden_sums ? align256((size_t)p.hidden_splits * rows * dim * 4) : 0;
   p.sums_w = p.weight_splits > 1 ? align256((size_t)p.weight_splits * p.piece * dim * 4) : 0;
   p.row_scale = align256((size_t)rows * 4);
@@ -438,24 +456,26 @@ struct Room {  // hands out a workspace
   }
 };
 
-// Whether the products can read the caller's own memory: 16-bit elements, rows of whole 16-byte chunks.
-static bool as_it_is(const void* p, int dim, int dtype) { return dtype != kF32 && dim % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+// Whether the products can read the caller's own memory: whole elements, rows of whole 16-byte chunks.
+static bool as_it_is(const void* p, int dim, int dtype, int64_t rows) {
+  return operand_planes(rows, dtype) == 1 && dim % (dtype == kF32 ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
 
 // An operand as the products see it, and what has to be laid out for that.
 static Matrix laid(const void* from, int64_t rows, int dim, void* room, bool own, Lay* l) {
   const int ld = ld_of(dim);
-  *l = {from, static_cast<unsigned short*>(room), rows, own ? 0 : (rows * ld / 8 + 255) / 256};
+  *l = {from, room, rows, own ? 0 : (rows * ld / 8 + 255) / 256};
   if (own) return {from, rows, dim, 0};
   return {room, rows, ld, rows * ld};
 }
-template <typename T>
+template <typename T, bool SPLIT>
 static void prepare(const XentArgs& a, const Lay& h, const Lay& w, const Scales& c, hipStream_t st) {
   const int64_t blocks = h.blocks + w.blocks + c.blocks;
-  if (blocks) hipLaunchKernelGGL(xent_prepare_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, a, h, w, ld_of(a.dim), c);
+  if (blocks) hipLaunchKernelGGL((xent_prepare_kernel<T, SPLIT>), dim3((unsigned)blocks), dim3(256), 0, st, a, h, w, ld_of(a.dim), c);
 }
 
-// T: element type of the arguments, E: of the products' operands
-template <typename T, typename E>
+// T: element type of the arguments, E: of the products' operands, PLANES: of dz (3: of the operands too)
+template <typename T, typename E, int PLANES>
 static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
   Room room{static_cast<char*>(a.ws)};
@@ -469,7 +489,7 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
   ProductArgs g{};
   Lay lh, lw;
-  g.b = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), &lh);
+  g.b = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype, a.rows), &lh);
   g.N = a.rows;
   g.K = a.dim;
   g.splits = p.fwd_splits;
@@ -478,7 +498,7 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   g.part = part;
   g.parts = p.parts;
   g.picked = picked;
-  const bool own = as_it_is(w, a.dim, dtype);
+  const bool own = as_it_is(w, a.dim, dtype, a.rows);
   const ProductPlan& plan = kPlans[p.fwd_shape];
   // (all classes at once where nothing is laid out, but no more blocks than a grid may have)
   const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 22) / ((a.rows + plan.bn - 1) / plan.bn)) * plan.bm;
@@ -487,12 +507,12 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   for (int64_t v0 = 0; v0 < a.classes && e == hipSuccess; v0 += piece) {
     const int64_t count = std::min(piece, a.classes - v0);
     g.a = laid(w + v0 * a.dim, count, a.dim, lay_w, own, &lw);
-    prepare<T>(a, lh, lw, Scales{}, st);
+    prepare<T, PLANES == 3>(a, lh, lw, Scales{}, st);
     lh.blocks = 0;
     g.M = count;
     g.v0 = v0;
     g.part0 = v0 / plan.bm * plan.wm;
-    e = launch_product<E, T>(kLogits, p.fwd_splits > 1 ? kSums : kForward, p.fwd_shape, g, st);
+    e = launch_product<E, T, PLANES>(kLogits, p.fwd_splits > 1 ? kSums : kForward, p.fwd_shape, g, st);
   }
   if (e != hipSuccess) return e;
   int team = 64;
@@ -531,7 +551,7 @@ static void xent_out(const float* sums, int splits, int64_t n, const float* scal
   hipLaunchKernelGGL(xent_out_kernel<T>, dim3(blocks), dim3(256), 0, st, sums, splits, n, scale, team, out);
 }
 
-template <typename T, typename E>
+template <typename T, typename E, int PLANES>
 static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
   Room room{static_cast<char*>(a.ws)};
@@ -546,13 +566,13 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
     hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a.up, a.rows, scale + 1);
   Scales scales{scale + 1, row_scale, keep, scale, half, (a.rows + 255) / 256};
   Lay lh, lw;
-  const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype), &lh);
-  const bool own = as_it_is(w, a.dim, dtype);
+  const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(h, a.dim, dtype, a.rows), &lh);
+  const bool own = as_it_is(w, a.dim, dtype, a.rows);
   hipError_t e = hipSuccess;
   for (int64_t v0 = 0; v0 < a.classes; v0 += p.piece) {
     const int64_t count = std::min(p.piece, a.classes - v0), ld = up_to(count, 8);
     const Matrix wm = laid(w + v0 * a.dim, count, a.dim, lay_w, own, &lw);
-    prepare<T>(a, lh, lw, scales, st);
+    prepare<T, PLANES == 3>(a, lh, lw, scales, st);
     lh.blocks = scales.blocks = 0;
     const Matrix zm{dz, a.rows, ld, a.rows * ld};
     ProductArgs g{};
@@ -561,19 +581,21 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
     g.a = wm; g.b = hm; g.M = count; g.N = a.rows; g.K = a.dim; g.splits = p.splits; g.sums = sums_z; g.add = 0;
     g.labels = a.labels; g.ignore = a.ignore; g.v0 = v0; g.stats = a.stats; g.row_scale = row_scale;
     g.dz = dz; g.dz_ld = ld; g.dz_plane = a.rows * ld;
-    if ((e = launch_product<E, T>(kLogits, p.splits > 1 ? kSums : kBackward, p.shape, g, st)) != hipSuccess) return e;
+    e = p.splits > 1 ? launch_product<E, T, PLANES == 2 ? 1 : PLANES>(kLogits, kSums, p.shape, g, st)
+                     : launch_product<E, T, PLANES>(kLogits, kBackward, p.shape, g, st);
+    if (e != hipSuccess) return e;
     if (p.splits > 1) {
       const unsigned blocks = (unsigned)std::min<int64_t>((a.rows * ld + 255) / 256, 4096);
-      hipLaunchKernelGGL((xent_dz_kernel<E, sizeof(T) == 4 ? 3 : 1>), dim3(blocks), dim3(256), 0, st, a, sums_z, p.splits, v0, count,
-                         ld, row_scale, static_cast<unsigned short*>(dz));
+      hipLaunchKernelGGL((xent_dz_kernel<E, PLANES>), dim3(blocks), dim3(256), 0, st, a, sums_z, p.splits, v0, count, ld, row_scale,
+                         static_cast<E*>(dz));
     }
     if (a.dh) {
       g.a = wm; g.b = zm; g.M = a.dim; g.N = a.rows; g.K = count;
-      g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape, planes_of(dtype) == 1 ? 1 : 6));
+      g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape, PLANES == 3 ? 6 : PLANES, 128 / (int)sizeof(E)));
       g.sums = p.hidden_sums ? sums_h : nullptr;
       g.add = v0 > 0;
       g.out = a.dh;
-      if ((e = launch_product<E, T>(kHidden, 0, p.hidden_shape, g, st)) != hipSuccess) return e;
+      if ((e = launch_product<E, T, PLANES>(kHidden, 0, p.hidden_shape, g, st)) != hipSuccess) return e;
     }
     if (a.dw) {
       T* out = static_cast<T*>(a.dw) + v0 * a.dim;
@@ -582,7 +604,7 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
       g.sums = p.weight_splits > 1 ? sums_w : nullptr;
       g.add = 0;
       g.out = out;
-      if ((e = launch_product<E, T>(kWeight, 0, p.weight_shape, g, st)) != hipSuccess) return e;
+      if ((e = launch_product<E, T, PLANES>(kWeight, 0, p.weight_shape, g, st)) != hipSuccess) return e;
       if (g.sums) xent_out(sums_w, p.weight_splits, count * a.dim, scale, out, st);
     }
   }
@@ -590,15 +612,13 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
-  return dtype == kF32   ? xent_fwd<float, bf16_t>(a, dtype, st)
-         : dtype == kF16 ? xent_fwd<half_t, half_t>(a, dtype, st)
-                         : xent_fwd<bf16_t, bf16_t>(a, dtype, st);
-}
-hipError_t launch_xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
-  return dtype == kF32   ? xent_bwd<float, bf16_t>(a, dtype, st)
-         : dtype == kF16 ? xent_bwd<half_t, half_t>(a, dtype, st)
-                         : xent_bwd<bf16_t, bf16_t>(a, dtype, st);
-}
+#define ECC_GO(WAY, TWO)                                                                                                       \
+  if (dtype == kF32) return native(a.rows, dtype) ? WAY<float, float, 1>(a, dtype, st) : WAY<float, bf16_t, 3>(a, dtype, st); \
+  const bool few = gradient_planes(a.rows, dtype) == 2;                                                                   \
+  if (dtype == kF16) return few ? WAY<half_t, half_t, TWO>(a, dtype, st) : WAY<half_t, half_t, 1>(a, dtype, st);            \
+  return few ? WAY<bf16_t, bf16_t, TWO>(a, dtype, st) : WAY<bf16_t, bf16_t, 1>(a, dtype, st)
+hipError_t launch_xent_fwd(const XentArgs& a, int dtype, hipStream_t st) { ECC_GO(xent_fwd, 1); }
+hipError_t launch_xent_bwd(const XentArgs& a, int dtype, hipStream_t st) { ECC_GO(xent_bwd, 2); }
+#undef ECC_GO
 
 }  // namespace ecc

@@ -1,0 +1,6 @@
+// Products of the linear head's cross entropy for float16 and few rows.
+#include "ecc_xent_launch.h"
+
+namespace ecc {
+template hipError_t launch_product<half_t, half_t, 2>(int, int, int, ProductArgs, hipStream_t);
+}

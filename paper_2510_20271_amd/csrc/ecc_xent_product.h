@@ -1,4 +1,4 @@
-// The matrix products of the linear head's cross entropy on the matrix cores, for 16-bit elements summed in float32:
+// The matrix products of the linear head's cross entropy on the matrix cores, summed in float32:
 //   kLogits  C[v][i] = sum_k W[v][k] H[i][k]    logits of a tile, consumed where they are made: a maximum and a sum for each
 //                                               row (forward), or their gradient dz (backward)
 //   kHidden  C[k][i] = sum_v W[v][k] dZ[i][v]   gradient of hidden
@@ -7,9 +7,12 @@
 // column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4, so a lane has a row's logits side by side (their maximum and sum need
 // no exchange but one between two lanes) and four neighbours along a result's row (stores of 8 or 16 bytes).
 //
-// float32 operands are three bfloat16 planes, x = x1 + x2 + x3, each the leading 8 bits of what is left: exact.  A product is
-// then six products of planes, x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1; what is left out is below 2^-23 of |x| |y|.  Six
-// bfloat16 instructions stand against sixteen times the float32 instruction's rate.
+// Elements are 16-bit, or float32 by the float32 instruction where rows are few (memory bounds those), or float32 as three
+// bfloat16 planes, x = x1 + x2 + x3, each the leading 8 bits of what is left: exact.  A product is then six products of planes,
+// x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1; what is left out is below 2^-23 of |x| |y|.  Six bfloat16 instructions stand
+// against sixteen times the float32 instruction's rate.  Where rows are few 16-bit gradients dz have a second plane as well, what
+// the first one's rounding left: over many rows that rounding (2^-9 of each dz for bfloat16, as much as the result's own) averages
+// out, over a few it need not.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -21,9 +24,10 @@ namespace ecc {
 constexpr int kLogits = 0, kHidden = 1, kWeight = 2;
 // of kLogits: what is made of them; kSums: nothing yet, their sums are split
 constexpr int kBackward = 0, kForward = 1, kSums = 2;
-constexpr int kDepth = 64;  // of a tile along the summed axis
+// elements of a tile along the summed axis: 128 bytes
+template <typename T> constexpr int kDepth = 128 / (int)sizeof(T);
 
-// A matrix of 16-bit elements [planes][rows][ld], ld a multiple of 8, 16-byte aligned; elements between a row's end and ld are 0.
+// A matrix [planes][rows][ld], rows of whole 16-byte chunks, 16-byte aligned; elements between a row's end and ld are 0.
 struct Matrix {
   const void* p;
   int64_t rows, ld, plane;  // plane: elements from one plane to the next
@@ -62,6 +66,9 @@ template <> struct Lanes<bf16_t> {
 template <> struct Lanes<half_t> {
   using V8 = _Float16 __attribute__((ext_vector_type(8)));
 };
+template <> struct Lanes<float> {
+  using V8 = float __attribute__((ext_vector_type(4)));  // (of a step of 8: half the lanes have the other four)
+};
 using Acc = float __attribute__((ext_vector_type(16)));
 using Quad = short __attribute__((ext_vector_type(4)));
 using LdsVoid = __attribute__((address_space(3))) void;
@@ -71,6 +78,12 @@ __device__ __forceinline__ Acc mma(Lanes<bf16_t>::V8 a, Lanes<bf16_t>::V8 b, Acc
 }
 __device__ __forceinline__ Acc mma(Lanes<half_t>::V8 a, Lanes<half_t>::V8 b, Acc c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ Acc mma(Lanes<float>::V8 a, Lanes<float>::V8 b, Acc c) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[k], b[k], c, 0, 0, 0);
+  return c;
 }
 
 // x as three bfloat16 values that add up to it.  They have the sign of x, and where x is not 0 none is: an empty one is the
@@ -95,27 +108,27 @@ __device__ __forceinline__ void split3(float x, unsigned short (&p)[3]) {
 constexpr int kFar = 0x7fffff00;       // an offset that no buffer holds: such a lane's 16 bytes read as zeros
 constexpr int64_t kReach = 0x40000000;  // what a tile's offsets stay below
 
-// One operand's tile in LDS, SIDE x kDepth, and how a wave fetches and reads it.  Fetches go straight to LDS, 1 KB a wave
+// One operand's tile in LDS, SIDE x kDepth<T>, and how a wave fetches and reads it.  Fetches go straight to LDS, 1 KB a wave
 // instruction, to consecutive 16-byte chunks; which chunk of its row a lane fetches is permuted so that reading is free of bank
 // conflicts.
-// ALONG: the operand's rows run along the summed axis: rows of 64 elements, two of which fill the banks, chunk c of row r at
+// ALONG: the operand's rows run along the summed axis: rows of 128 bytes, two of which fill the banks, chunk c of row r at
 // place c ^ (r / 2 & 7): 16 lanes read one chunk of 16 rows at a time.
-// Otherwise the tile has 64 rows of SIDE elements, and is read through the transposing LDS read: 16 lanes get 16 neighbouring
+// Otherwise the tile has kDepth rows of SIDE elements.  float32 is read element by element; 16-bit elements are read through the transposing LDS read: 16 lanes get 16 neighbouring
 // elements of 4 rows, transposed.  Four rows and their 64 bytes fill the banks once: chunk c of row r at c ^ 4 (r & 3) (for
 // rows of 128 bytes, of which two fill the banks, c ^ 4 (r / 2 & 1); rows of 64 bytes as they are).
 // where an operand's next tile is, uniform over the block
-template <bool ALONG>
+template <typename T, bool ALONG>
 struct Cursor {
   const char* at;
   int64_t left;  // bytes of the operand from there
   int64_t step;  // bytes to the next tile
   int64_t plane;
   __device__ __forceinline__ Cursor(const Matrix& m, int64_t origin, int64_t K, int k0) {
-    const int64_t first = ALONG ? origin * m.ld : (int64_t)k0 * kDepth * m.ld + origin;
-    at = static_cast<const char*>(m.p) + first * 2;
-    left = ((ALONG ? m.rows : K) * m.ld - first) * 2;
-    step = ALONG ? 0 : (int64_t)kDepth * m.ld * 2;
-    plane = m.plane * 2;
+    const int64_t first = ALONG ? origin * m.ld : (int64_t)k0 * kDepth<T> * m.ld + origin;
+    at = static_cast<const char*>(m.p) + first * (int64_t)sizeof(T);
+    left = ((ALONG ? m.rows : K) * m.ld - first) * (int64_t)sizeof(T);
+    step = ALONG ? 0 : (int64_t)128 * m.ld;
+    plane = m.plane * (int64_t)sizeof(T);
   }
   __device__ __forceinline__ int reach() const { return (int)(left < 0 ? 0 : left < kReach ? left : kReach); }
   __device__ __forceinline__ void next() {
@@ -126,18 +139,20 @@ struct Cursor {
 
 template <typename T, bool ALONG, int SIDE, int WAVES>
 struct Tile {
-  static constexpr int kBytes = SIDE * kDepth * 2;
+  static constexpr int kBytes = SIDE * 128;
   static constexpr int kFetches = kBytes / 1024;
   static constexpr int kEach = kFetches / WAVES;
   static_assert(kFetches % WAVES == 0, "every wave fetches alike");
-  static constexpr int kRow = ALONG ? 8 : SIDE / 8;  // chunks of a row
-  static constexpr int kReads = ALONG ? 1 : 2;       // LDS instructions of an operand
+  static constexpr int kRow = ALONG ? 8 : SIDE * (int)sizeof(T) / 16;   // chunks of a row
+  static constexpr int kReads = ALONG ? 1 : sizeof(T) == 4 ? 4 : 2;     // LDS instructions of an operand
+  static constexpr int kPer = 16 / (int)sizeof(T);                      // elements of a chunk
   using V8 = typename Lanes<T>::V8;
   int offset[kEach];  // of this lane's chunk, in bytes from the tile's origin
   int mark[kEach];    // ALONG: the chunk's first element along the summed axis; otherwise its row
 
   __device__ __forceinline__ static int place(int row, int c) {
     if (ALONG) return c ^ (row >> 1 & 7);
+    if (sizeof(T) == 4) return c;
     if (kRow >= 16) return c ^ ((row & 3) << 2);
     if (kRow == 8) return c ^ ((row >> 1 & 1) << 2);
     return c;
@@ -147,9 +162,9 @@ struct Tile {
 #pragma unroll
     for (int f = 0; f < kEach; ++f) {
       const int at = (wave * kEach + f) * 64 + lane, row = at / kRow, c = place(row, at % kRow);
-      offset[f] = (int)(row * m.ld * 2) + c * 16;
-      mark[f] = ALONG ? c * 8 : row;
-      if (!ALONG && origin + c * 8 >= m.ld) offset[f] = kFar;
+      offset[f] = (int)(row * m.ld * (int)sizeof(T)) + c * 16;
+      mark[f] = ALONG ? c * kPer : row;
+      if (!ALONG && origin + c * kPer >= m.ld) offset[f] = kFar;
     }
   }
   // A tile to LDS at `to`: the tile's origin is at `from`, which `left` bytes of the operand follow; k: its first element along
@@ -164,14 +179,21 @@ struct Tile {
       if (ALONG) at = mark[f] < end ? at : kFar;
       else at = (keep >> mark[f]) & 1 ? at : kFar;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)(to + (wave * kEach + f) * 1024), 16, at,
-                                               ALONG ? __builtin_amdgcn_readfirstlane(k * 2) : 0, 0, 0);
+                                               ALONG ? __builtin_amdgcn_readfirstlane(k * (int)sizeof(T)) : 0, 0, 0);
     }
   }
-  // operand of a matrix instruction: 32 rows / columns from `side`, 16 elements of the summed axis from 16 ks
+  // operand of a matrix instruction: 32 rows / columns from `side`, a quarter of the tile's elements along the summed axis
   __device__ __forceinline__ static V8 read(const unsigned char* from, int side, int ks, int lane) {
     if (ALONG) {
       const int row = side + (lane & 31);
       return *reinterpret_cast<const V8*>(from + row * 128 + place(row, ks * 2 + (lane >> 5)) * 16);
+    }
+    if constexpr (sizeof(T) == 4) {
+      V8 v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        v[k] = *reinterpret_cast<const float*>(from + ((ks * 8 + (lane >> 5) * 4 + k) * SIDE + side + (lane & 31)) * 4);
+      return v;
     }
     const int q = lane >> 4, i = lane & 15, row = ks * 16 + (q >> 1) * 8 + (i >> 2), col = side + (q & 1) * 16 + (i & 3) * 4;
     typedef __attribute__((address_space(3))) Quad LdsQuad;
@@ -268,7 +290,8 @@ __device__ __forceinline__ void wait_and_meet() {
 
 // O: element type of the result;  BM x BN: a block's tile of C, WM x WN waves;  STAGES: tiles in LDS, all but one of them on
 // their way (thin tiles are computed faster than one arrives)
-template <typename T, typename O, int KIND, int MODE, int BM, int BN, int WM, int WN, int STAGES>
+// PLANES: of dz; 3: of every operand
+template <typename T, typename O, int PLANES, int KIND, int MODE, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs g) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
@@ -279,7 +302,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   int tm, tn, split;
   tile_of((int)blockIdx.x, (int)gridDim.x, g.tiles_m, g.tiles_n, tm, tn, split);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-  constexpr int kPairs = sizeof(O) == 4 ? 6 : 1;  // products of planes
+  constexpr int kPairs = PLANES == 3 ? 6 : KIND == kLogits ? 1 : PLANES;  // products of planes
   const int k0 = split * g.steps, ktiles = min(g.steps, g.total - k0), turns = ktiles * kPairs;
   TA ta;
   TB tb;
@@ -292,24 +315,25 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   Acc total = {};
 
   // the next fetch: tile, pair of planes, and the rows that count (read a turn ahead)
-  Cursor<KIND == kLogits> ca(g.a, m0, g.K, k0);
-  Cursor<KIND != kWeight> cb(g.b, n0, g.K, k0);
+  Cursor<T, KIND == kLogits> ca(g.a, m0, g.K, k0);
+  Cursor<T, KIND != kWeight> cb(g.b, n0, g.K, k0);
   int lk = k0, lj = 0;
   const auto* rows = (const __attribute__((address_space(4))) unsigned long long*)g.keep;  // (scalar reads)
-  unsigned long long keep = KIND == kWeight ? rows[lk] : ~0ull;
+  const auto rows_at = [&](int k) { return rows[k * kDepth<T> / 64] >> (k * kDepth<T> % 64); };
+  unsigned long long keep = KIND == kWeight ? rows_at(lk) : ~0ull;
   const auto fetch = [&](int turn) {
-    // pairs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), two bits each
-    const int64_t pa = kPairs == 1 ? 0 : (0x0850 >> (2 * lj) & 3) * ca.plane, pb = kPairs == 1 ? 0 : (0x0244 >> (2 * lj) & 3) * cb.plane;
+    // pairs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), two bits each (two: (0,0) (0,1))
+    const int64_t pa = kPairs <= 2 ? 0 : (0x0850 >> (2 * lj) & 3) * ca.plane, pb = kPairs == 1 ? 0 : (0x0244 >> (2 * lj) & 3) * cb.plane;
     unsigned char* to = smem + turn % STAGES * kBoth;
     const bool any = turn < turns;  // (behind the last tile nothing is read: zeros go where no one looks)
-    ta.fetch(ca.at + pa, any ? ca.reach() : 0, (int)g.a.ld, lk * kDepth, to, wave, keep);
-    tb.fetch(cb.at + pb, any ? cb.reach() : 0, (int)g.b.ld, lk * kDepth, to + TA::kBytes, wave, ~0ull);
+    ta.fetch(ca.at + pa, any ? ca.reach() : 0, (int)g.a.ld, lk * kDepth<T>, to, wave, keep);
+    tb.fetch(cb.at + pb, any ? cb.reach() : 0, (int)g.b.ld, lk * kDepth<T>, to + TA::kBytes, wave, ~0ull);
     if (kPairs == 1 || ++lj == kPairs) {
       lj = 0;
       ++lk;
       ca.next();
       cb.next();
-      if (KIND == kWeight) keep = rows[min(lk, g.total - 1)];
+      if (KIND == kWeight) keep = rows_at(min(lk, g.total - 1));
     }
   };
   const int am = (wave % WM) * (BM / WM), bn = (wave / WM) * (BN / WN);
@@ -328,8 +352,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
     };
     read(0);
 #pragma unroll
-    for (int ks = 0; ks < kDepth / 16; ++ks) {
-      if (ks + 1 < kDepth / 16) read(ks + 1);
+    for (int ks = 0; ks < 4; ++ks) {
+      if (ks + 1 < 4) read(ks + 1);
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -409,29 +433,32 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
           const float p = row == want ? -miss : __expf((acc[i][j][r] - lse) - rest);
           acc[i][j][r] = counts && row < left ? p * scale : 0.0f;
         }
-      using Out = Turn<unsigned short, TM>;
+      using Out = Turn<T, TM>;
       unsigned char* room = smem + wave * Out::kBytes;
 #pragma unroll
-      for (int k = 0; k < (kPairs == 1 ? 1 : 3); ++k) {
+      for (int k = 0; k < PLANES; ++k) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            unsigned short e[4];
+            T e[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              if constexpr (kPairs == 1) {
-                e[r] = __builtin_bit_cast(unsigned short, narrow<T>(acc[i][j][q * 4 + r]));
-              } else {  // the leading 8 bits, and what is left for the next plane
-                const unsigned bits = __float_as_uint(acc[i][j][q * 4 + r]);
-                e[r] = (unsigned short)(bits >> 16);
-                acc[i][j][q * 4 + r] -= __uint_as_float(bits & 0xffff0000u);
+            for (int r = 0; r < 4; ++r) {  // (and what is left for the next plane)
+              float f = acc[i][j][q * 4 + r];
+              if constexpr (PLANES == 3) {
+                const unsigned bits = __float_as_uint(f);
+                e[r] = __builtin_bit_cast(T, (unsigned short)(bits >> 16));
+                f -= __uint_as_float(bits & 0xffff0000u);
+              } else {
+                e[r] = narrow<T>(f);
+                if (PLANES == 2) f -= widen(e[r]);
               }
+              acc[i][j][q * 4 + r] = f;
             }
             Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);
           }
         const int64_t first = n0 + bn + j * 32;
-        Out::store(room, lane, static_cast<unsigned short*>(g.dz) + k * g.dz_plane + first * g.dz_ld + m0 + am, g.dz_ld,
+        Out::store(room, lane, static_cast<T*>(g.dz) + k * g.dz_plane + first * g.dz_ld + m0 + am, g.dz_ld,
                    g.N - first, g.dz_ld - m0 - am, 16);
       }
     } else {
@@ -485,7 +512,7 @@ struct ProductPlan { int bm, bn, wm; };
 constexpr ProductPlan kPlans[] = {{256, 256, 2}, {128, 128, 2}, {128, 32, 4}, {32, 128, 1}, {64, 256, 1}};
 
 // g.a .. g.K, splits set; tiles, steps and total are filled in here
-template <typename T, typename O>
+template <typename T, typename O, int PLANES>
 hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStream_t st);
 
 }  // namespace ecc
