@@ -122,8 +122,9 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(XentArgs a, const float*
   const float* z = sums + (in ? row : 0) * a.classes;
   float m = -INFINITY, s = 0.0f;
   for (int64_t v = lane; v < a.classes; v += team) {
-    float x = z[v];
-    for (int k = 1; k < splits; ++k) x += z[k * all + v];
+    float x = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) x += z[k * all + v];
     if (in && v == label) picked[row] = x;
     const float top = fmaxf(m, x), base = top == -INFINITY ? 0.0f : top;
     s = s * __expf(m - base) + (v == label ? 0.0f : __expf(x - base));
@@ -347,7 +348,7 @@ constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 
 // float32: by the float32 instruction where rows are few and the weights' way from memory counts (41 x 2363 x 31381: step XENT_PLANES us
 // by planes, XENT_NATIVE so), by planes of bfloat16 otherwise.  16-bit: two planes of dz where rows are few.
-constexpr int64_t kFewRows = 96, kFewHalves = 64;
+constexpr int64_t kFewRows = 64, kFewHalves = 64;
 static bool native(int64_t rows, int dtype) { return dtype == kF32 && rows <= kFewRows; }
 static int operand_planes(int64_t rows, int dtype) { return dtype == kF32 && !native(rows, dtype) ? 3 : 1; }
 static int gradient_planes(int64_t rows, int dtype) {
@@ -361,6 +362,7 @@ static int ld_of(int dim) { return (int)up_to(dim, 8); }
 static int shape_of(int64_t M, int64_t N, int64_t runs, int64_t turns, bool few = false) {
   if (N <= 32) return 2;
   if (M <= 32) return 3;
+  if (N <= 64) return 5;
   if (M <= 64 && N > 128) return 4;
   const int64_t large = (M + 255) / 256 * ((N + 255) / 256);
   return !few && M > 128 && N > 128 && turns >= 8 && large * runs >= 256 ? 0 : 1;
@@ -412,7 +414,7 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   p.shape = shape_of(p.piece, rows, 1, dim_turns, few);
   // logits by split sums: where their tiles leave compute units idle through a long sum
   const auto split = [&](int64_t M, int shape) {
-    const int splits = dim_turns < 16 || M > 4096 ? 1 : splits_of(M, rows, dim, shape, pairs, depth);
+    const int splits = dim_turns < 16 || M > 1024 ? 1 : splits_of(M, rows, dim, shape, pairs, depth);
     return splits >= 4 ? splits : 1;
   };
   p.fwd_splits = classes <= p.fwd_piece ? split(classes, p.fwd_shape) : 1;

@@ -63,8 +63,10 @@ hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStrea
     case 3: return turns == 1  ? product_shape<T, O, PLANES, 32, 128, 1, 4, 1>(kind, mode, g, st)
                    : turns < 4 ? product_shape<T, O, PLANES, 32, 128, 1, 4, 2>(kind, mode, g, st)
                                : product_shape<T, O, PLANES, 32, 128, 1, 4, 4>(kind, mode, g, st);
-    default: return turns == 1 ? product_shape<T, O, PLANES, 64, 256, 1, 4, 1>(kind, mode, g, st)
-                               : product_shape<T, O, PLANES, 64, 256, 1, 4, 2>(kind, mode, g, st);
+    case 4: return turns == 1 ? product_shape<T, O, PLANES, 64, 256, 1, 4, 1>(kind, mode, g, st)
+                              : product_shape<T, O, PLANES, 64, 256, 1, 4, 2>(kind, mode, g, st);
+    default: return turns == 1 ? product_shape<T, O, PLANES, 128, 64, 4, 1, 1>(kind, mode, g, st)
+                               : product_shape<T, O, PLANES, 128, 64, 4, 1, 3>(kind, mode, g, st);
   }
 }
 

@@ -507,9 +507,10 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------------
-// Tiles: 0: 256 x 256 (8 waves, a block a CU), 1: 128 x 128 (4 waves, two blocks), 2: 128 x 32, 3: 32 x 128, 4: 64 x 256
+// Tiles: 0: 256 x 256 (8 waves, a block a CU), 1: 128 x 128 (4 waves, two blocks), 2: 128 x 32, 3: 32 x 128, 4: 64 x 256,
+// 5: 128 x 64
 struct ProductPlan { int bm, bn, wm; };
-constexpr ProductPlan kPlans[] = {{256, 256, 2}, {128, 128, 2}, {128, 32, 4}, {32, 128, 1}, {64, 256, 1}};
+constexpr ProductPlan kPlans[] = {{256, 256, 2}, {128, 128, 2}, {128, 32, 4}, {32, 128, 1}, {64, 256, 1}, {128, 64, 4}};
 
 // g.a .. g.K, splits set; tiles, steps and total are filled in here
 template <typename T, typename O, int PLANES>
