@@ -27,7 +27,7 @@ static hipError_t product_go(const ProductArgs& g, int threads, hipStream_t st) 
 template <typename T, typename O, int PLANES, int BM, int BN, int WM, int WN, int STAGES>
 static hipError_t product_shape(int kind, int mode, const ProductArgs& g, hipStream_t st) {
   constexpr int kShared = STAGES * (BM + BN) * 128, kThreads = WM * WN * 64;
-  if constexpr (PLANES != 2) {  // (forward logits and split sums know nothing of a second plane of dz)
+  if constexpr (PLANES != kTwo) {  // (forward logits and split sums know nothing of a second plane of dz)
     if (kind == kLogits && mode == kForward)
       return product_go<product_kernel<T, O, PLANES, kLogits, kForward, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
     if (kind == kLogits && mode == kSums)
@@ -47,13 +47,13 @@ hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStrea
   g.total = (int)((g.K + kDepth<T> - 1) / kDepth<T>);
   g.steps = (g.total + g.splits - 1) / g.splits;
   g.splits = (g.total + g.steps - 1) / g.steps;  // (no run is empty)
-  const int turns = g.steps * (PLANES == 3 ? 6 : kind == kLogits ? 1 : PLANES);
+  const int turns = g.steps * (PLANES == kBoth ? 3 : kind == kLogits ? 1 : PLANES);
   // One turn needs one tile in LDS, which leaves room for more blocks (385475 x 18 x 599 in float16: logits 176 us with two,
-  // 145 with one); thin tiles are four ahead where there are turns to come (32 x 128 x 1000 in float32 planes: 10.4 us with
-  // two, 7.8 with four).
+  // 145 with one); thin tiles are four ahead where there are turns to come (32 x 128 x 1000, 12 turns: 10.4 us with two, 7.8
+  // with four).
   switch (shape) {
     case 0:
-      if constexpr (PLANES != 2 && sizeof(T) == 2) return product_shape<T, O, PLANES, 256, 256, 2, 4, 2>(kind, mode, g, st);
+      if constexpr (PLANES != kTwo && sizeof(T) == 2) return product_shape<T, O, PLANES, 256, 256, 2, 4, 2>(kind, mode, g, st);
       return hipErrorInvalidValue;  // (few rows: not asked for)
     case 1: return turns == 1 ? product_shape<T, O, PLANES, 128, 128, 2, 2, 1>(kind, mode, g, st)
                               : product_shape<T, O, PLANES, 128, 128, 2, 2, 2>(kind, mode, g, st);

@@ -7,12 +7,13 @@
 // column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4, so a lane has a row's logits side by side (their maximum and sum need
 // no exchange but one between two lanes) and four neighbours along a result's row (stores of 8 or 16 bytes).
 //
-// Elements are 16-bit, or float32 by the float32 instruction where rows are few (memory bounds those), or float32 as three
-// bfloat16 planes, x = x1 + x2 + x3, each the leading 8 bits of what is left: exact.  A product is then six products of planes,
-// x1 y1 + x1 y2 + x2 y1 + x2 y2 + x1 y3 + x3 y1; what is left out is below 2^-23 of |x| |y|.  Six bfloat16 instructions stand
-// against sixteen times the float32 instruction's rate.  Where rows are few 16-bit gradients dz have a second plane as well, what
-// the first one's rounding left: over many rows that rounding (2^-9 of each dz for bfloat16, as much as the result's own) averages
-// out, over a few it need not.
+// Elements are 16-bit, or float32 by the float32 instruction where rows are few (memory bounds those), or float32 as two float16
+// planes: x s = x1 + x2 with s the power of two that brings the operand's largest value to 2^14 .. 2^15, x1 the nearest float16
+// and x2 the nearest to what is left, good to 2^-23 of x and 2^-39 of the largest.  A product is then three products of planes,
+// x1 y1 + x1 y2 + x2 y1; x2 y2, left out, is of random sign and below 2^-22 of |x| |y| (2^-25 at the middle).  Three float16
+// instructions stand against sixteen times the float32 instruction's rate.
+// Where rows are few 16-bit gradients dz have a second plane as well, what the first one's rounding left: over many rows that
+// rounding (2^-9 of each dz for bfloat16, as much as the result's own) averages out, over a few it need not.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -45,7 +46,8 @@ struct ProductArgs {
   float* sums;         // kHidden, kWeight, kSums: [splits][N][M], or null: straight to out
   int add;             //   added to what is there
   void* out;           // [N][M], scaled by *scale
-  const float* scale;
+  const float* scale;  // [1]
+  const float* unscale;  // [1], kBoth: what logits are multiplied by
   // kLogits
   const int64_t* labels;
   int64_t v0;          // the first class of this piece (M: its classes)
@@ -86,24 +88,9 @@ __device__ __forceinline__ Acc mma(Lanes<float>::V8 a, Lanes<float>::V8 b, Acc c
   return c;
 }
 
-// x as three bfloat16 values that add up to it.  They have the sign of x, and where x is not 0 none is: an empty one is the
-// least normal number, so that an Inf meets no zero in the six products that its own product does not (Inf times x is an Inf
-// of the right sign; the error is 2^-126 and counts for nothing).  NaN: NaN and zeros.
-__device__ __forceinline__ void split3(float x, unsigned short (&p)[3]) {
-  const unsigned bits = __float_as_uint(x);
-  const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
-  const float r1 = finite ? x - __uint_as_float(bits & 0xffff0000u) : 0.0f;
-  const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
-  p[0] = (unsigned short)(bits >> 16);
-  p[1] = (unsigned short)(__float_as_uint(r1) >> 16);
-  p[2] = (unsigned short)(__float_as_uint(r2) >> 16);
-  if (!finite && (bits & 0x007fffffu)) p[0] = 0x7fc0;
-  else if (p[0] & 0x7fff) {
-    const unsigned short least = (unsigned short)((p[0] & 0x8000) | 0x0080);
-    if (!(p[1] & 0x7fff)) p[1] = least;
-    if (!(p[2] & 0x7fff)) p[2] = least;
-  }
-}
+// PLANES of the products: one of everything; two of dz; two of dz and of the operands
+constexpr int kOne = 1, kTwo = 2, kBoth = 3;
+constexpr int planes_of_dz(int planes) { return planes == kOne ? 1 : 2; }
 
 constexpr int kFar = 0x7fffff00;       // an offset that no buffer holds: such a lane's 16 bytes read as zeros
 constexpr int64_t kReach = 0x40000000;  // what a tile's offsets stay below
@@ -290,19 +277,19 @@ __device__ __forceinline__ void wait_and_meet() {
 
 // O: element type of the result;  BM x BN: a block's tile of C, WM x WN waves;  STAGES: tiles in LDS, all but one of them on
 // their way (thin tiles are computed faster than one arrives)
-// PLANES: of dz; 3: of every operand
+// PLANES: kOne, kTwo, kBoth
 template <typename T, typename O, int PLANES, int KIND, int MODE, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs g) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
   using TA = Tile<T, KIND == kLogits, BM, kWaves>;
   using TB = Tile<T, KIND != kWeight, BN, kWaves>;
-  constexpr int kBoth = TA::kBytes + TB::kBytes;
+  constexpr int kStage = TA::kBytes + TB::kBytes;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int tm, tn, split;
   tile_of((int)blockIdx.x, (int)gridDim.x, g.tiles_m, g.tiles_n, tm, tn, split);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-  constexpr int kPairs = PLANES == 3 ? 6 : KIND == kLogits ? 1 : PLANES;  // products of planes
+  constexpr int kPairs = PLANES == kBoth ? 3 : KIND == kLogits ? 1 : PLANES;  // products of planes
   const int k0 = split * g.steps, ktiles = min(g.steps, g.total - k0), turns = ktiles * kPairs;
   TA ta;
   TB tb;
@@ -322,9 +309,9 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   const auto rows_at = [&](int k) { return rows[k * kDepth<T> / 64] >> (k * kDepth<T> % 64); };
   unsigned long long keep = KIND == kWeight ? rows_at(lk) : ~0ull;
   const auto fetch = [&](int turn) {
-    // pairs (0,0) (0,1) (1,0) (1,1) (0,2) (2,0), two bits each (two: (0,0) (0,1))
-    const int64_t pa = kPairs <= 2 ? 0 : (0x0850 >> (2 * lj) & 3) * ca.plane, pb = kPairs == 1 ? 0 : (0x0244 >> (2 * lj) & 3) * cb.plane;
-    unsigned char* to = smem + turn % STAGES * kBoth;
+    // pairs (0,0) (0,1) (1,0)
+    const int64_t pa = kPairs == 3 && lj == 2 ? ca.plane : 0, pb = kPairs > 1 && lj == 1 ? cb.plane : 0;
+    unsigned char* to = smem + turn % STAGES * kStage;
     const bool any = turn < turns;  // (behind the last tile nothing is read: zeros go where no one looks)
     ta.fetch(ca.at + pa, any ? ca.reach() : 0, (int)g.a.ld, lk * kDepth<T>, to, wave, keep);
     tb.fetch(cb.at + pb, any ? cb.reach() : 0, (int)g.b.ld, lk * kDepth<T>, to + TA::kBytes, wave, ~0ull);
@@ -342,7 +329,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   for (int t = 0; t < (STAGES > 1 ? STAGES - 1 : 1); ++t) fetch(t);
   for (int t = 0; t < turns; ++t) {
     wait_and_meet<STAGES < 3 ? 0 : (STAGES - 2) * (TA::kEach + TB::kEach)>();  // the tile is there, and the one before has been read
-    const unsigned char* from = smem + t % STAGES * kBoth;
+    const unsigned char* from = smem + t % STAGES * kStage;
     typename TA::V8 a[2][TM], b[2][TN];
     const auto read = [&](int ks) {
 #pragma unroll
@@ -375,6 +362,15 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   }
   wait_and_meet<0>();  // the last fetches have landed and the tiles are read: LDS is free
 
+  if constexpr (PLANES == kBoth && KIND == kLogits && MODE != kSums) {
+    const float by = *g.unscale;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] *= by;
+  }
   const int rows0 = 4 * (lane >> 5);  // accumulator r is row 8 (r / 4) + rows0 + r % 4 of its 32
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
@@ -436,7 +432,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
       using Out = Turn<T, TM>;
       unsigned char* room = smem + wave * Out::kBytes;
 #pragma unroll
-      for (int k = 0; k < PLANES; ++k) {
+      for (int k = 0; k < planes_of_dz(PLANES); ++k) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -445,14 +441,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
 #pragma unroll
             for (int r = 0; r < 4; ++r) {  // (and what is left for the next plane)
               float f = acc[i][j][q * 4 + r];
-              if constexpr (PLANES == 3) {
-                const unsigned bits = __float_as_uint(f);
-                e[r] = __builtin_bit_cast(T, (unsigned short)(bits >> 16));
-                f -= __uint_as_float(bits & 0xffff0000u);
-              } else {
-                e[r] = narrow<T>(f);
-                if (PLANES == 2) f -= widen(e[r]);
-              }
+              e[r] = narrow<T>(f);
+              if (PLANES != kOne) f -= widen(e[r]);
               acc[i][j][q * 4 + r] = f;
             }
             Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);

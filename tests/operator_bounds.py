@@ -78,6 +78,12 @@ def xent_reference(h, W, labels, ignore, reduction, up=None):
     z = h @ W.t()
     # float32 products of at most 24 + 24 bits, summed in some order
     d_z = (4 * math.sqrt(d) + 4) * E * (h.abs() @ W.abs().t())
+    # float32 with more than 128 rows, 128 classes and 2^29 products: two float16 planes, each value good to 2^-23 of itself and 2^-39
+    # of the largest, products of the second planes (2^-11 each, at most) left out: 2 2^-23 + 2^-22 = 8 E of a product
+    planes = dtype == torch.float32 and min(n, V) > 128 and n * d * V > 2 ** 29
+    floor = 2.0 ** -39 * planes
+    top_h, top_w, extra = h.abs().max(), W.abs().max(), 8 * E * planes
+    d_z = d_z + extra * (h.abs() @ W.abs().t()) + floor * (top_h * W.abs().sum(1)[None, :] + top_w * h.abs().sum(1, keepdim=True))
     lse = torch.logsumexp(z, 1, keepdim=True)
     top_d = d_z.amax(1, keepdim=True)
     rows = (lse - z.gather(1, at))[:, 0]
@@ -98,14 +104,15 @@ def xent_reference(h, W, labels, ignore, reduction, up=None):
     # exp of a difference that is off by d_z + what lse is off by; then held in the type (float32: whole)
     off = d_z + top_d + 8 * E * (1 + z.abs() + lse.abs())
     d_dz = (p * torch.expm1(off) + 4 * E * (p + hit)) * g.abs() + rounding(dz, torch.float32 if dtype == torch.float32 else dtype) * (dz != 0)
+    d_dz = d_dz + planes * (2 * E * dz.abs() + floor * g.abs().max() * (g != 0))
     d_dz = d_dz + 4 * 2.0 ** -126 * g.abs()  # (what is below the least normal number may be taken as 0)
     if dtype == torch.float16:  # held as a multiple of the largest upstream gradient by 2^-14
         d_dz = d_dz.clamp_max(1e30) - rounding(dz, dtype) * (dz != 0) + torch.finfo(dtype).eps / 2 * (
             dz.abs() + g.abs().max() * 2.0 ** -28) * (dz != 0)
     sums_v, sums_n = (4 * math.sqrt(V) + 8) * E, (4 * math.sqrt(n) + 8) * E
     dh, dW = dz @ W, dz.t() @ h
-    d_dh = d_dz @ W.abs() + sums_v * (dz.abs() @ W.abs()) + rounding(dh, dtype)
-    d_dW = d_dz.t() @ h.abs() + sums_n * (dz.abs().t() @ h.abs()) + rounding(dW, dtype)
+    d_dh = d_dz @ W.abs() + (sums_v + extra) * (dz.abs() @ W.abs()) + floor * top_w * dz.abs().sum(1, keepdim=True) + rounding(dh, dtype)
+    d_dW = d_dz.t() @ h.abs() + (sums_n + extra) * (dz.abs().t() @ h.abs()) + floor * top_h * dz.abs().sum(0)[:, None] + rounding(dW, dtype)
     return loss, d_loss, dh, d_dh, dW, d_dW
 
 

@@ -13,7 +13,7 @@ F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
 SHAPES = [  # rows, dim, classes
     (1, 1, 1), (1, 1, 2), (2, 3, 5), (1, 64, 1000), (7, 16, 21), (64, 64, 64), (33, 30, 257), (129, 65, 131), (300, 128, 1000),
     (1000, 8, 3), (17, 2050, 33), (5, 40, 20011), (520, 264, 300), (2100, 72, 21), (256, 512, 512), (1, 4096, 3001),
-    (70, 100, 8200), (4099, 33, 70),
+    (70, 100, 8200), (4099, 33, 70), (1030, 263, 2050), (9000, 1100, 60), (200, 3001, 1000),
 ]
 
 
@@ -59,7 +59,7 @@ def test_reductions(n, d, V, dtype, reduction):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("n,d,V", [(4, 8, 6), (300, 64, 500)])
+@pytest.mark.parametrize("n,d,V", [(4, 8, 6), (300, 64, 500), (300, 902, 2100)])
 def test_rows_left_out(n, d, V, dtype):
     h, W, labels, up = _data(n, d, V, dtype, seed=4)
     # all of them: no loss and no gradient
@@ -76,7 +76,7 @@ def test_rows_left_out(n, d, V, dtype):
     clean = h.clone()
     for bad in (float("nan"), float("inf"), -float("inf")):
         h[1] = bad
-        h[1, 0] = 0.0
+        h[1, 0] = 1e30
         want = api.ecc_xent_fwd(clean, W, labels)
         got = api.ecc_xent_fwd(h, W, labels)
         assert torch.equal(want[0], got[0]) and torch.equal(want[2], got[2])
@@ -111,18 +111,20 @@ def test_large_logits_do_not_overflow(dtype):
     _check(h, low, labels % 5 + (labels < 0) * -100, "mean", up)
 
 
-def test_infinite_logits():
-    """A weight of -inf takes its class out of the sum; a logit of +inf or NaN leaves no finite loss."""
-    h = torch.ones(3, 4, device="cuda")
-    W = torch.randn(9, 4, device="cuda", generator=torch.Generator("cuda").manual_seed(0))
-    labels = torch.tensor([0, 1, 2], device="cuda")
+@pytest.mark.parametrize("n,d,V", [(3, 4, 8), (300, 4, 8), (300, 904, 2000)])
+def test_infinite_logits(n, d, V):
+    """A weight of -inf takes its class out of the sum; a logit of +inf or NaN leaves no finite loss.  (With such weights the
+    float32 planes are cut off instead of rounded: products of second planes of 2^-10 each are left out, 2^-20 of logits of size 1.)"""
+    h = torch.ones(n, d, device="cuda")
+    W = torch.randn(V + 1, d, device="cuda", generator=torch.Generator("cuda").manual_seed(0)) * d ** -0.5
+    labels = torch.arange(n, device="cuda") % V
     gone = W.clone()
-    gone[8] = -float("inf")
-    want = api.ecc_xent_fwd(h, W[:8].contiguous(), labels, reduction="none")[0]
+    gone[V] = -float("inf")
+    want = api.ecc_xent_fwd(h, W[:V].contiguous(), labels, reduction="none")[0]
     got = api.ecc_xent_fwd(h, gone, labels, reduction="none")[0]
-    assert float((want - got).abs().max()) < 1e-6
+    assert float((want - got).abs().max()) < 1e-5
     for bad in (float("inf"), float("nan")):
-        gone[8] = bad
+        gone[V] = bad
         assert not bool(torch.isfinite(api.ecc_xent_fwd(h, gone, labels, reduction="none")[0]).any())
 
 
@@ -150,7 +152,7 @@ def test_layouts(dtype):
             assert bool((t[:shift] == 7).all()) and bool((t[shift + size:] == 7).all())
 
 
-@pytest.mark.parametrize("n,d,V,dtype", [(300, 64, 900, BF16), (40, 50, 3000, F32), (3000, 32, 20, F16)])
+@pytest.mark.parametrize("n,d,V,dtype", [(300, 64, 900, BF16), (40, 50, 3000, F32), (3000, 32, 20, F16), (700, 500, 1700, F32)])
 def test_same_bits_again_and_one_gradient_alone(n, d, V, dtype):
     h, W, labels, up = _data(n, d, V, dtype, seed=8)
     loss, stats, counted = api.ecc_xent_fwd(h, W, labels)
@@ -340,3 +342,19 @@ def test_features_beyond_32_bits():
         size += p.abs().t() @ hd.abs()
     # dz rounded to bfloat16 (2^-9, independent over 3e7 rows: 4 / sqrt(n) of the sizes' sum) and float32 sums in runs
     assert bool(((dW.double() - want).abs() <= 2.0 ** -8 * want.abs() + size * (4 * 2.0 ** -9 / n ** 0.5 + 1e-5)).all())
+
+
+@pytest.mark.parametrize("scale_h,scale_w", [(1e-20, 1e15), (3e4, 1e-6), (1e18, 1e-18), (1e-30, 1e-30), (0.0, 1.0)])
+def test_float32_of_any_size(scale_h, scale_w):
+    """The planes' scales follow the operands: largest values from 1e-30 to 1e18, and none but zeros."""
+    for n, d, V in ((60, 40, 90), (150, 1000, 4000)):
+        h, W, labels, up = _data(n, d, V, F32, seed=16)
+        _check(h * scale_h, W * scale_w, labels, "sum", up)
+
+
+def test_float32_rows_of_different_sizes():
+    """Rows and classes between 1 and 2^-12 of the largest."""
+    h, W, labels, up = _data(300, 1000, 2000, F32, seed=17)
+    h = h * 2.0 ** -(torch.arange(300, device="cuda") % 13)[:, None]
+    W = W * 2.0 ** -(torch.arange(2000, device="cuda") % 13)[:, None]
+    _check(h, W, labels, "none", up * 2.0 ** -(torch.arange(300, device="cuda") % 11))
