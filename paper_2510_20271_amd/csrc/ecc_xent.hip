@@ -249,13 +249,13 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(XentArgs a, const float*
   const bool in = row < a.rows;
   const int64_t all = a.rows * a.classes, label = in ? a.labels[row] : -1;
   const float* z = sums + (in ? row : 0) * a.classes;
-  const float by = unscale ? *unscale : 1.0f;
+  const float by = unscale ? unscale[0] : 1.0f, by2 = unscale ? unscale[1] : 1.0f;
   float m = -INFINITY, s = 0.0f;
   for (int64_t v = lane; v < a.classes; v += team) {
     float x = 0.0f;
 #pragma unroll 4
     for (int k = 0; k < splits; ++k) x += z[k * all + v];
-    x *= by;
+    x = x * by * by2;
     if (in && v == label) picked[row] = x;
     const float top = fmaxf(m, x), base = top == -INFINITY ? 0.0f : top;
     s = s * __expf(m - base) + (v == label ? 0.0f : __expf(x - base));
@@ -273,14 +273,14 @@ template <typename E, int PLANES>
 __global__ __launch_bounds__(256) void xent_dz_kernel(XentArgs a, const float* sums, int splits, int64_t v0, int64_t count, int64_t ld,
                                                       const float* row_scale, const float* unscale, E* dz) {
   const int64_t all = a.rows * ld, n = a.rows * count;
-  const float by = unscale ? *unscale : 1.0f;
+  const float by = unscale ? unscale[0] : 1.0f, by2 = unscale ? unscale[1] : 1.0f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / ld, v = i - row * ld, label = a.labels[row];
     float f = 0.0f;
     if (v < count && label != a.ignore) {
       float x = sums[row * count + v];
       for (int k = 1; k < splits; ++k) x += sums[k * n + row * count + v];
-      x *= by;
+      x = x * by * by2;
       const double lse = a.stats[row * 2];
       const float high = (float)lse, low = (float)(lse - (double)high);
       f = (v0 + v == label ? -(float)a.stats[row * 2 + 1] : __expf((x - high) - low)) * row_scale[row];
@@ -383,12 +383,15 @@ __global__ __launch_bounds__(64) void xent_total_kernel(XentArgs a, const RowSum
   if (threadIdx.x == 0) xent_finish(a, s, n);
 }
 
-// the largest |upstream gradient|, in one block: only where float16 meets a gradient for each row
-__global__ __launch_bounds__(kSumThreads) void xent_top_kernel(const float* up, int64_t rows, float* top) {
+// the largest finite |upstream gradient| of the rows that count, in one block: only where float16 meets a gradient for each row
+__global__ __launch_bounds__(kSumThreads) void xent_top_kernel(XentArgs a, float* top) {
   __shared__ float part[kSumThreads / 64];
   float m = 0.0f;
 #pragma unroll 8
-  for (int64_t i = threadIdx.x; i < rows; i += kSumThreads) m = fmaxf(m, fabsf(up[i]));
+  for (int64_t i = threadIdx.x; i < a.rows; i += kSumThreads) {
+    const float v = fabsf(a.up[i]);
+    if (v < INFINITY && a.labels[i] != a.ignore) m = fmaxf(m, v);
+  }
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
   __syncthreads();
@@ -402,18 +405,22 @@ struct Scales {
   const float* top;  // float16 planes with a gradient for each row: the largest of them
   float* row_scale;  // null: forward
   unsigned long long* keep;
-  float* scale;      // [3]: of the gradient of hidden, of the weight's, of logits
+  float* scale;      // [4]: of the gradient of hidden, of the weight's, of logits (two factors: one could overflow)
   bool half;         // dz is held in float16
   int64_t blocks;    // 0: none wanted
 };
 __device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, int64_t block, int exponent_h, int exponent_w) {
   const int64_t i = block * 256 + threadIdx.x;
-  if (i == 0) c.scale[2] = (float)ldexp(1.0, -exponent_h - exponent_w);
+  if (i == 0) {
+    const int exponent = -exponent_h - exponent_w;
+    c.scale[2] = ldexpf(1.0f, exponent / 2);
+    c.scale[3] = ldexpf(1.0f, exponent - exponent / 2);
+  }
   if (!c.row_scale) return;
   float by = c.half ? kHalfScale : 1.0f, back = 1.0f / by;
   if (a.reduction == kEach) {
     if (c.half) {
-      const float t = c.top[0] > 0.0f ? c.top[0] : 1.0f;
+      const float t = c.top[0] > 0.0f ? fmaxf(c.top[0], 0x1p-100f) : 1.0f;  // (kHalfScale / t stays finite)
       by /= t;
       back *= t;
     }
@@ -735,8 +742,8 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   const bool half = dtype == kF16 || PLANES == kBoth;
   const float* unscale = PLANES == kBoth ? scale + 2 : nullptr;
   if (half && a.reduction == kEach)
-    hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a.up, a.rows, scale + 3);
-  Scales scales{scale + 3, row_scale, keep, scale, half, (a.rows + 255) / 256};
+    hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a, scale + 4);
+  Scales scales{scale + 4, row_scale, keep, scale, half, (a.rows + 255) / 256};
   Lay lh, lw;
   const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(a, h, dtype), &lh);
   const bool own = as_it_is(a, w, dtype);

@@ -47,7 +47,7 @@ struct ProductArgs {
   int add;             //   added to what is there
   void* out;           // [N][M], scaled by *scale
   const float* scale;  // [1]
-  const float* unscale;  // [1], kBoth: what logits are multiplied by
+  const float* unscale;  // [2], kBoth: what logits are multiplied by
   // kLogits
   const int64_t* labels;
   int64_t v0;          // the first class of this piece (M: its classes)
@@ -363,13 +363,13 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   wait_and_meet<0>();  // the last fetches have landed and the tiles are read: LDS is free
 
   if constexpr (PLANES == kBoth && KIND == kLogits && MODE != kSums) {
-    const float by = *g.unscale;
+    const float by = g.unscale[0], by2 = g.unscale[1];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] *= by;
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = acc[i][j][r] * by * by2;
   }
   const int rows0 = 4 * (lane >> 5);  // accumulator r is row 8 (r / 4) + rows0 + r % 4 of its 32
 #pragma unroll

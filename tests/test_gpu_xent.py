@@ -358,3 +358,37 @@ def test_float32_rows_of_different_sizes():
     h = h * 2.0 ** -(torch.arange(300, device="cuda") % 13)[:, None]
     W = W * 2.0 ** -(torch.arange(2000, device="cuda") % 13)[:, None]
     _check(h, W, labels, "none", up * 2.0 ** -(torch.arange(300, device="cuda") % 11))
+
+
+@pytest.mark.parametrize("n,d,V,dtype", [(30, 8, 12, F16), (300, 904, 2000, F16), (300, 904, 2000, F32)])
+def test_upstream_gradients_of_rows_do_not_reach_others(n, d, V, dtype):
+    """dz in float16 is a multiple of the largest upstream gradient: of the rows that count, and finite."""
+    h, W, labels, up = _data(n, d, V, dtype, seed=31)
+    labels[:2] = torch.tensor([1, -100])
+    want = torch.autograd.grad(linear_cross_entropy(h.requires_grad_(True), W.requires_grad_(True), labels, reduction="none"), (h, W), up)
+
+    def again(up):
+        return torch.autograd.grad(linear_cross_entropy(h, W, labels, reduction="none"), (h, W), up)
+
+    far = up.clone()
+    far[1] = 1e30  # a row that is left out
+    assert all(torch.equal(a, b) for a, b in zip(again(far), want))
+    far[0] = float("inf")
+    got = again(far)[0]
+    assert not bool(torch.isfinite(got[0]).all())
+    # (another largest one: another multiple, 2^-11 of each dz, and its sums)
+    ref = xent_reference(h.detach(), W.detach(), labels, -100, "none", up)
+    within(got[1:], ref[2][1:], ref[3][1:], "dhidden")
+    if dtype == F32:  # (2^-114: a subnormal result is good to 2^-149, 2^-35 of 1; dz below 2^-100 2^-39 is 0, 2^-25 of 1, over V and n)
+        for a, b, terms in zip(again(up * 2.0 ** -114), want, (W.abs().sum(0).max(), h.abs().sum(0).max())):
+            assert bool((a.double() * 2.0 ** 114 - b.double()).abs().max() <= 2.0 ** -23 * terms + 1e-5 * b.abs().max())
+
+
+def test_float32_products_beyond_its_range():
+    """A row of zeros among features and weights whose products overflow: log V, not 0 times infinity."""
+    h, W, labels, _ = _data(300, 904, 2000, F32, seed=32, ignored=0.0)
+    h, W = h * 1e30, W * 1e30
+    h[5] = 0.0
+    loss = api.ecc_xent_fwd(h, W, labels, reduction="none")[0]
+    want = xent_reference(h[5:6], W, labels[5:6], -100, "none", torch.ones(1, device="cuda"))
+    within(loss[5:6], want[0], want[1], "loss")
