@@ -7,10 +7,10 @@
 // column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4, so a lane has a row's logits side by side (their maximum and sum need
 // no exchange but one between two lanes) and four neighbours along a result's row (stores of 8 or 16 bytes).
 //
-// Elements are 16-bit, or float32 by the float32 instruction where rows are few (memory bounds those), or float32 as two float16
-// planes: x s = x1 + x2 with s the power of two that brings the operand's largest value to 2^14 .. 2^15, x1 the nearest float16
-// and x2 the nearest to what is left, good to 2^-23 of x and 2^-39 of the largest.  A product is then three products of planes,
-// x1 y1 + x1 y2 + x2 y1; x2 y2, left out, is of random sign and below 2^-22 of |x| |y| (2^-25 at the middle).  Three float16
+// Elements are 16-bit, or float32 by the float32 instruction where rows or classes are few (memory bounds those) or all is small, or
+// float32 as two float16 planes: x s = x1 + x2 with s the power of two that brings the operand's largest value to 2^14 .. 2^15, x1 the
+// nearest float16 and x2 the nearest to what is left, good to 2^-23 of x and 2^-39 of the largest.  A product is then three products
+// of planes, x1 y1 + x1 y2 + x2 y1; x2 y2, left out, is of random sign and below 2^-22 of |x| |y| (2^-25 at the middle).  Three float16
 // instructions stand against sixteen times the float32 instruction's rate.
 // Where rows are few 16-bit gradients dz have a second plane as well, what the first one's rounding left: over many rows that
 // rounding (2^-9 of each dz for bfloat16, as much as the result's own) averages out, over a few it need not.
