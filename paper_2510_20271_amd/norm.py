@@ -47,18 +47,17 @@ def group_norm_act(x, groups: int, weight=None, bias=None, eps: float = 1e-5, ac
     channels = x.shape[-1]
     if channels < 1 or int(groups) < 1 or channels % int(groups):
         raise ValueError(f"groups must divide the {channels} channels, got {groups}")
+    code = api._one_of(api._ACTS, act, "act")
+    api._one_of(api._OPERATOR_DTYPES, x.dtype, "the type of x")
     for name, t in (("weight", weight), ("bias", bias)):
         if t is not None and tuple(t.shape) != (channels,):
             raise ValueError(f"{name} must have {channels} elements, got shape {tuple(t.shape)}")
+        if t is not None and t.device != x.device:
+            raise ValueError(f"{name} must be on {x.device}, got {t.device}")
     if x.numel() == 0:  # no item or no point: nothing to normalise, gradients of zero
         return x * 1.0 + sum(t.sum().to(x.dtype) * 0.0 for t in (weight, bias) if t is not None)
     weight = None if weight is None else weight.float().contiguous()
     bias = None if bias is None else bias.float().contiguous()
-    code = api._one_of(api._ACTS, act, "act")
-    api._one_of(api._OPERATOR_DTYPES, x.dtype, "the type of x")
-    for name, t in (("weight", weight), ("bias", bias)):
-        if t is not None and t.device != x.device:
-            raise ValueError(f"{name} must be on {x.device}, got {t.device}")
     x = x.contiguous()
     with api._on_device_of(x):
         if _plain(x, weight, bias):

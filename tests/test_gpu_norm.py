@@ -271,3 +271,36 @@ def test_features_beyond_32_bits():
     m2 = spread((dw * w).view(G, -1).sum(1) / m)
     want = spread(rstd) * (dv * w - m1 - xhat * m2)
     assert bool(((gx[0, -100:].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all())
+
+
+def test_refusals_of_empty_features():
+    x = torch.zeros(0, 5, 12, device="cuda")
+    for call in (lambda: group_norm_act(x, 3, act="tanh"), lambda: group_norm_act(x.int(), 3),
+                 lambda: group_norm_act(x, 3, torch.ones(12))):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_more_items_than_a_launch_takes():
+    """Curves of eight thresholds: a block an item, in several launches."""
+    n, T = 2 ** 25 + 70000, 8
+    gen = torch.Generator("cuda").manual_seed(40)
+    x = torch.randn(n, T, generator=gen, device="cuda", dtype=BF16)
+    dy = torch.randn(n, T, generator=gen, device="cuda", dtype=BF16)
+    w, b = 1 + torch.rand(T, generator=gen, device="cuda"), torch.rand(T, generator=gen, device="cuda")
+    y, stats = api.ecc_norm_fwd(x, 2, w, b, act="none")
+    dx, dw, db = api.ecc_norm_bwd(x, dy, 2, stats, w, b, act="none")
+    for at in (0, 2 ** 24 - 50, 2 ** 25 - 50, n - 100):
+        _, st = api.ecc_norm_fwd(x[at:at + 100].contiguous(), 2, w, b, act="none")
+        some = api.ecc_norm_bwd(x[at:at + 100].contiguous(), dy[at:at + 100].contiguous(), 2, st, w, b, act="none")
+        assert torch.equal(stats[at:at + 100], st) and torch.equal(dx[at:at + 100], some[0])
+        assert torch.equal(y[at:at + 100], api.ecc_norm_fwd(x[at:at + 100].contiguous(), 2, w, b, act="none")[0])
+    want_w, want_b, size_w, size_b = (torch.zeros(T, device="cuda", dtype=torch.float64) for _ in range(4))
+    for k in range(0, n, 2 ** 22):
+        g = dy[k:k + 2 ** 22].double()
+        st = stats[k:k + 2 ** 22].repeat_interleave(T // 2, 1)
+        t = g * (x[k:k + 2 ** 22].double() - st[..., 0]) * st[..., 1]
+        want_w += t.sum(0); want_b += g.sum(0); size_w += t.abs().sum(0); size_b += g.abs().sum(0)
+    # (a row's term is float32: a few roundings; the rows' sums are float64)
+    assert bool(((dw.double() - want_w).abs() <= 2.0 ** -21 * size_w).all())
+    assert bool(((db.double() - want_b).abs() <= 2.0 ** -21 * size_b).all())
