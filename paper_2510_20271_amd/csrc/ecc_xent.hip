@@ -31,17 +31,48 @@ struct Lay {
   void* to;
   int64_t rows, blocks;
 };
-template <typename T>
-__device__ __forceinline__ void lay_chunk(const Lay& l, int dim, int ld, int64_t block) {
-  const int64_t at = (block * 256 + threadIdx.x) * 8, all = l.rows * ld;
-  if (at >= all) return;
-  const int64_t row = at / ld;
-  const int k = (int)(at - row * ld);
-  using Bits = typename std::conditional<sizeof(T) == 4, unsigned, unsigned short>::type;
-  struct alignas(16) Eight { Bits e[8]; } w;
+// A thread lays out chunks of 8 elements: of row `row` from element k.  Rows start anywhere, so whole chunks are fetched at the
+// alignment of an element (8 fetches of an element each: 72 us for 125 MB of float32, 47 so).
+constexpr int kLayTurns = 4;
+template <typename GO>
+__device__ __forceinline__ void lay_turns(const Lay& l, int ld, int64_t block, GO&& go) {
+  const int64_t all = l.rows * ld, at = (block * kLayTurns * 256 + threadIdx.x) * 8;
+  const int hop = 256 * 8 / ld, move = 256 * 8 - hop * ld;  // rows and elements from one turn to the next
+  int64_t row = at / ld;
+  int k = (int)(at - row * ld);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w.e[i] = k + i < dim ? static_cast<const Bits*>(l.from)[row * dim + k + i] : (Bits)0;
-  *reinterpret_cast<Eight*>(static_cast<Bits*>(l.to) + at) = w;
+  for (int t = 0; t < kLayTurns; ++t) {
+    if (at + t * 256 * 8 >= all) return;
+    go(row, k, at + t * 256 * 8);
+    row += hop;
+    k += move;
+    if (k >= ld) {
+      k -= ld;
+      ++row;
+    }
+  }
+}
+template <typename T>
+struct Eight { T e[8]; };
+template <typename T>
+__device__ __forceinline__ Eight<T> eight_of(const Lay& l, int dim, int64_t row, int k) {
+  const T* from = static_cast<const T*>(l.from) + row * dim + k;
+  Eight<T> w;
+  if (k + 8 <= dim) {
+    __builtin_memcpy(&w, from, sizeof(w));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w.e[i] = k + i < dim ? from[i] : (T)0;
+  }
+  return w;
+}
+template <typename T>
+__device__ __forceinline__ void lay_chunks(const Lay& l, int dim, int ld, int64_t block) {
+  using Bits = typename std::conditional<sizeof(T) == 4, unsigned, unsigned short>::type;
+  lay_turns(l, ld, block, [&](int64_t row, int k, int64_t at) {
+    const Eight<Bits> w = eight_of<Bits>(l, dim, row, k);
+    __builtin_memcpy(__builtin_assume_aligned(static_cast<Bits*>(l.to) + at, 16), &w, sizeof(w));
+  });
 }
 
 // ---- float32 as planes of float16 --------------------------------------------------------------------------------------------
@@ -168,23 +199,17 @@ __device__ __forceinline__ void split2(float x, bool wild, half_t& high, half_t&
     if ((float)low == 0.0f) low = least;
   }
 }
-constexpr int kLayTurns = 4;  // chunks of 8 a thread
 __device__ __forceinline__ void lay_planes(const Lay& l, int dim, int ld, int64_t block, int exponent, bool wild) {
-  const int64_t all = l.rows * ld;
   const float by = ldexpf(1.0f, exponent);
-  const float* from = static_cast<const float*>(l.from);
+  const int64_t all = l.rows * ld;
+  lay_turns(l, ld, block, [&](int64_t row, int k, int64_t at) {
+    const Eight<float> x = eight_of<float>(l, dim, row, k);
+    Eight<half_t> high, low;
 #pragma unroll
-  for (int t = 0; t < kLayTurns; ++t) {
-    const int64_t at = ((block * kLayTurns + t) * 256 + threadIdx.x) * 8;
-    if (at >= all) return;
-    const int64_t row = at / ld;
-    const int k = (int)(at - row * ld);
-    struct alignas(16) Eight { half_t e[8]; } high, low;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) split2(k + i < dim ? from[row * dim + k + i] * by : 0.0f, wild, high.e[i], low.e[i]);
-    *reinterpret_cast<Eight*>(static_cast<half_t*>(l.to) + at) = high;
-    *reinterpret_cast<Eight*>(static_cast<half_t*>(l.to) + all + at) = low;
-  }
+    for (int i = 0; i < 8; ++i) split2(x.e[i] * by, wild, high.e[i], low.e[i]);
+    __builtin_memcpy(__builtin_assume_aligned(static_cast<half_t*>(l.to) + at, 16), &high, 16);
+    __builtin_memcpy(__builtin_assume_aligned(static_cast<half_t*>(l.to) + all + at, 16), &low, 16);
+  });
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------
@@ -448,9 +473,9 @@ __device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, i
 template <typename T>
 __global__ __launch_bounds__(256) void xent_prepare_kernel(XentArgs a, Lay h, Lay w, int ld, Scales c) {
   int64_t block = blockIdx.x;
-  if (block < h.blocks) return lay_chunk<T>(h, a.dim, ld, block);
+  if (block < h.blocks) return lay_chunks<T>(h, a.dim, ld, block);
   block -= h.blocks;
-  if (block < w.blocks) return lay_chunk<T>(w, a.dim, ld, block);
+  if (block < w.blocks) return lay_chunks<T>(w, a.dim, ld, block);
   scale_rows(a, c, block - w.blocks, 0, 0);
 }
 __global__ __launch_bounds__(256) void xent_prepare_planes_kernel(XentArgs a, Lay h, Lay w, int ld, Scales c, const Range* part,
@@ -494,6 +519,7 @@ __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int sp
 
 // ---- plans -----------------------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of a plane of dz, and of laid-out weights: what the Infinity Cache holds
+constexpr int64_t kPieceFew = (int64_t)1 << 30;      // of laid-out weights where rows are few
 constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
 constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 
@@ -564,7 +590,11 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   const int64_t dim_turns = (dim + depth - 1) / depth * pairs;
   p.fwd_shape = shape_of(classes, rows, 1, dim_turns, few);
   p.parts = (classes + kPlans[p.fwd_shape].bm - 1) / kPlans[p.fwd_shape].bm * kPlans[p.fwd_shape].wm;
-  p.fwd_piece = pieces(std::min(kPieceMost * 8, kPieceBytes / (ld * size)));
+  // (few rows: pieces of as many tiles as the card holds blocks, within kPieceFew; 38 x 2030 x 92507 in float32: products 485 us by
+  // pieces of kPieceBytes, 266 so)
+  const int64_t tiles = (rows + kPlans[p.fwd_shape].bn - 1) / kPlans[p.fwd_shape].bn;
+  const int64_t full = std::min((512 + tiles - 1) / tiles * kPlans[p.fwd_shape].bm, kPieceFew / (ld * size));
+  p.fwd_piece = pieces(std::min(kPieceMost * 8, std::max(full, kPieceBytes / (ld * size))));
   p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * size), way == kBoth ? kPieceBytes / (ld * size) : kPieceMost}));
   p.ld_dz = up_to(p.piece, 8);
   p.shape = shape_of(p.piece, rows, 1, dim_turns, few);
@@ -624,20 +654,18 @@ static bool as_it_is(const XentArgs& a, const void* p, int dtype) {
 // An operand as the products see it, and what has to be laid out for that.
 static Matrix laid(const void* from, int64_t rows, int dim, void* room, bool own, Lay* l) {
   const int ld = ld_of(dim);
-  *l = {from, room, rows, own ? 0 : (rows * ld / 8 + 255) / 256};
+  *l = {from, room, rows, own ? 0 : (rows * ld / 8 + 256 * kLayTurns - 1) / (256 * kLayTurns)};
   if (own) return {from, rows, dim, 0};
   return {room, rows, ld, rows * ld};
 }
 // blocks that look for an operand's range: 16 values a thread or more
 static int range_blocks(int64_t n) { return (int)std::max<int64_t>(1, std::min<int64_t>(kRangeBlocks, n / 4096)); }
 template <typename T, int PLANES>
-static void prepare(const XentArgs& a, Lay h, Lay w, const Scales& c, Range* range, hipStream_t st) {
+static void prepare(const XentArgs& a, const Lay& h, const Lay& w, const Scales& c, Range* range, hipStream_t st) {
   if constexpr (PLANES == kBoth) {
     const int bh = range_blocks(a.rows * a.dim), bw = range_blocks(a.classes * a.dim);
     if (c.blocks)  // (the first piece)
       hipLaunchKernelGGL(xent_range_kernel, dim3((unsigned)(bh + bw)), dim3(256), 0, st, a, bh, range);
-    h.blocks = (h.blocks + kLayTurns - 1) / kLayTurns;
-    w.blocks = (w.blocks + kLayTurns - 1) / kLayTurns;
     hipLaunchKernelGGL(xent_prepare_planes_kernel, dim3((unsigned)(h.blocks + w.blocks + c.blocks)), dim3(256), 0, st, a, h, w,
                        ld_of(a.dim), c, range, bh, bw);
   } else {
