@@ -523,13 +523,13 @@ constexpr int64_t kPieceFew = (int64_t)1 << 30;      // of laid-out weights wher
 constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
 constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 
-// float32: by the float32 instruction where rows or classes are a tile or fewer, where the operands' way from memory counts (steps: 100
-// rows x 2364 x 31381 713 us so, 1227 by planes; 200 rows, a second tile, about 1400 so, 1344 by planes; 100000 x 512 x 100 564 so,
-// 719 by planes), and where the whole is so small that two launches more count (502 x 102 x 18, the loss alone: 18 us so, 40 by
-// planes); by planes of float16 otherwise.  16-bit: two planes of dz where rows are few.
+// float32: by the float32 instruction where rows or classes are a tile or fewer, where the operands' way from memory counts (steps: 128
+// rows x 2364 x 31381 753 us so, 939 by planes; 200 rows, a second tile, 1229 so, 1039 by planes; 100000 x 512 x 100 545 so, 573 by
+// planes), and where the whole is so small that two launches more count (502 x 102 x 18, the loss alone: 20 us so, 24 by planes; 400 x
+// 511 x 2000, step: 216 so, 182 by planes); by planes of float16 otherwise.  16-bit: two planes of dz where rows are few.
 static bool few_rows(int64_t rows, int64_t dim, int64_t classes, int dtype) {
   if (dtype != kF32) return rows <= 64;
-  return rows <= 128 || classes <= 128 || rows * dim <= ((int64_t)1 << 29) / classes;
+  return rows <= 128 || classes <= 128 || rows * dim <= ((int64_t)1 << 28) / classes;
 }
 static int way_of(int64_t rows, int64_t dim, int64_t classes, int dtype) {
   const bool few = few_rows(rows, dim, classes, dtype);

@@ -78,9 +78,9 @@ def xent_reference(h, W, labels, ignore, reduction, up=None):
     z = h @ W.t()
     # float32 products of at most 24 + 24 bits, summed in some order
     d_z = (4 * math.sqrt(d) + 4) * E * (h.abs() @ W.abs().t())
-    # float32 with more than 128 rows, 128 classes and 2^29 products: two float16 planes, each value good to 2^-23 of itself and 2^-39
+    # float32 with more than 128 rows, 128 classes and 2^28 products: two float16 planes, each value good to 2^-23 of itself and 2^-39
     # of the largest, products of the second planes (2^-11 each, at most) left out: 2 2^-23 + 2^-22 = 8 E of a product
-    planes = dtype == torch.float32 and min(n, V) > 128 and n * d * V > 2 ** 29
+    planes = dtype == torch.float32 and min(n, V) > 128 and n * d * V > 2 ** 28
     floor = 2.0 ** -39 * planes
     top_h, top_w, extra = h.abs().max(), W.abs().max(), 8 * E * planes
     d_z = d_z + extra * (h.abs() @ W.abs().t()) + floor * (top_h * W.abs().sum(1)[None, :] + top_w * h.abs().sum(1, keepdim=True))
