@@ -761,7 +761,9 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
   Room room{static_cast<char*>(a.ws)};
   void *lay_h = room.take(p.lay_h), *lay_w = room.take(p.lay_w), *dz = room.take(p.dz);
-  float *sums_z = static_cast<float*>(room.take(p.sums_z)), *sums_h = static_cast<float*>(room.take(p.sums_h)), *sums_w = static_cast<float*>(room.take(p.sums_w));
+  float* sums_z = static_cast<float*>(room.take(p.sums_z));
+  float* sums_h = static_cast<float*>(room.take(p.sums_h));
+  float* sums_w = static_cast<float*>(room.take(p.sums_w));
   float* row_scale = static_cast<float*>(room.take(p.row_scale));
   unsigned long long* keep = static_cast<unsigned long long*>(room.take(p.keep));
   Range* range = static_cast<Range*>(room.take(p.range));

@@ -100,7 +100,8 @@ constexpr int64_t kReach = 0x40000000;  // what a tile's offsets stay below
 // conflicts.
 // ALONG: the operand's rows run along the summed axis: rows of 128 bytes, two of which fill the banks, chunk c of row r at
 // place c ^ (r / 2 & 7): 16 lanes read one chunk of 16 rows at a time.
-// Otherwise the tile has kDepth rows of SIDE elements.  float32 is read element by element; 16-bit elements are read through the transposing LDS read: 16 lanes get 16 neighbouring
+// Otherwise the tile has kDepth rows of SIDE elements.  float32 is read element by element; 16-bit elements are read through
+// the transposing LDS read: 16 lanes get 16 neighbouring
 // elements of 4 rows, transposed.  Four rows and their 64 bytes fill the banks once: chunk c of row r at c ^ 4 (r & 3) (for
 // rows of 128 bytes, of which two fill the banks, c ^ 4 (r / 2 & 1); rows of 64 bytes as they are).
 // where an operand's next tile is, uniform over the block
