@@ -17,7 +17,7 @@ namespace ecc {
 
 // float16 (a type of its own, or float32's planes) holds dz as a multiple of 2^-14 of the largest upstream gradient: the probabilities
 // of a large vocabulary are far below its least number otherwise.  (They are at most 1: 2^14 is in range.  Values are good to 2^-39 of
-// the largest; in one plane what is below 2^-28 of it loses digits of its own.)
+// the largest.)
 constexpr float kHalfScale = 16384.0f;
 
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -526,14 +526,14 @@ constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 // float32: by the float32 instruction where rows or classes are a tile or fewer, where the operands' way from memory counts (steps: 128
 // rows x 2364 x 31381 753 us so, 939 by planes; 200 rows, a second tile, 1229 so, 1039 by planes; 100000 x 512 x 100 545 so, 573 by
 // planes), and where the whole is so small that two launches more count (502 x 102 x 18, the loss alone: 20 us so, 24 by planes; 400 x
-// 511 x 2000, step: 216 so, 182 by planes); by planes of float16 otherwise.  16-bit: two planes of dz where rows are few.
+// 511 x 2000, step: 216 so, 182 by planes); by planes of float16 otherwise.  16-bit: two planes of dz.
 static bool few_rows(int64_t rows, int64_t dim, int64_t classes, int dtype) {
-  if (dtype != kF32) return rows <= 64;
+  if (dtype != kF32) return false;
   return rows <= 128 || classes <= 128 || rows * dim <= ((int64_t)1 << 28) / classes;
 }
 static int way_of(int64_t rows, int64_t dim, int64_t classes, int dtype) {
   const bool few = few_rows(rows, dim, classes, dtype);
-  return dtype == kF32 ? (few ? kOne : kBoth) : few ? kTwo : kOne;
+  return dtype == kF32 ? (few ? kOne : kBoth) : kTwo;
 }
 static int ld_of(int dim) { return (int)up_to(dim, 8); }
 
@@ -823,11 +823,11 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   return hipGetLastError();
 }
 
-#define ECC_GO(WAY, FEW)                                                                                                  \
-  const bool few = few_rows(a.rows, a.dim, a.classes, dtype);                                                              \
-  if (dtype == kF32) return few ? WAY<float, float, kOne>(a, dtype, st) : WAY<float, half_t, kBoth>(a, dtype, st);         \
-  if (dtype == kF16) return few ? WAY<half_t, half_t, FEW>(a, dtype, st) : WAY<half_t, half_t, kOne>(a, dtype, st);        \
-  return few ? WAY<bf16_t, bf16_t, FEW>(a, dtype, st) : WAY<bf16_t, bf16_t, kOne>(a, dtype, st)
+#define ECC_GO(WAY, PLANES)                                                                                               \
+  if (dtype == kF32)                                                                                                       \
+    return few_rows(a.rows, a.dim, a.classes, dtype) ? WAY<float, float, kOne>(a, dtype, st)                               \
+                                                     : WAY<float, half_t, kBoth>(a, dtype, st);                            \
+  return dtype == kF16 ? WAY<half_t, half_t, PLANES>(a, dtype, st) : WAY<bf16_t, bf16_t, PLANES>(a, dtype, st)
 hipError_t launch_xent_fwd(const XentArgs& a, int dtype, hipStream_t st) { ECC_GO(xent_fwd, kOne); }
 hipError_t launch_xent_bwd(const XentArgs& a, int dtype, hipStream_t st) { ECC_GO(xent_bwd, kTwo); }
 #undef ECC_GO

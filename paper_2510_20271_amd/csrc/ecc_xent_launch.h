@@ -53,8 +53,8 @@ hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStrea
   // with four).
   switch (shape) {
     case 0:
-      if constexpr (PLANES != kTwo && sizeof(T) == 2) return product_shape<T, O, PLANES, 256, 256, 2, 4, 2>(kind, mode, g, st);
-      return hipErrorInvalidValue;  // (few rows: not asked for)
+      if constexpr (sizeof(T) == 2) return product_shape<T, O, PLANES, 256, 256, 2, 4, 2>(kind, mode, g, st);
+      return hipErrorInvalidValue;  // (float32: not asked for)
     case 1: return turns == 1 ? product_shape<T, O, PLANES, 128, 128, 2, 2, 1>(kind, mode, g, st)
                               : product_shape<T, O, PLANES, 128, 128, 2, 2, 2>(kind, mode, g, st);
     case 2: return turns == 1  ? product_shape<T, O, PLANES, 128, 32, 4, 1, 1>(kind, mode, g, st)

@@ -12,8 +12,10 @@
 // nearest float16 and x2 the nearest to what is left, good to 2^-23 of x and 2^-39 of the largest.  A product is then three products
 // of planes, x1 y1 + x1 y2 + x2 y1; x2 y2, left out, is of random sign and below 2^-22 of |x| |y| (2^-25 at the middle).  Three float16
 // instructions stand against sixteen times the float32 instruction's rate.
-// Where rows are few 16-bit gradients dz have a second plane as well, what the first one's rounding left: over many rows that
-// rounding (2^-9 of each dz for bfloat16, as much as the result's own) averages out, over a few it need not.
+// 16-bit gradients dz have a second plane as well, what the first one's rounding left, so that the sums of them are off by no more than
+// float32 sums are: that rounding (2^-9 of each dz for bfloat16) is as much as the result's own, and neither sum averages it out, over
+// classes (hidden's gradient) or over rows, where one term is most of it.  It costs the two gradients' products twice the matrix
+// instructions (8192 x 4096 x 131072 bfloat16 step: 48.0 ms, 31.0 with one plane).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
