@@ -395,10 +395,8 @@ int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t point
  * ecc_xent_bwd: grad_loss (device float32, [1] or [rows] as the loss) carried on to grad_hidden and grad_weight (as hidden
  * and weight), either of which may be NULL.  Rows that are left out get zeros and, whatever their features hold, add
  * nothing to grad_weight.
- * Products are summed in float32.  16-bit types hold the logits' gradient to twice their bits (float16: and to 2^-39 of the largest
- * upstream gradient).  float32 with more than 128 rows, 128 classes and 2^28 products: operands and the logits' gradient are good to
- * 2^-23 of a value and 2^-39 of the operand's largest; otherwise they are whole.  Orders are fixed: repeated calls give the same
- * bits.
+ * Operands are multiplied as they are and summed in float32.  16-bit types hold the logits' gradient to twice their bits (float16: and
+ * to 2^-39 of the largest upstream gradient).  Orders are fixed: repeated calls give the same bits.
  *   1 <= rows, classes < 2^31, 1 <= dim <= ECC_MAX_CHANNELS;  workspace: 256-byte aligned, of ecc_xent_workspace_bytes()
  *   bytes (backward: 0 or 1)
  */

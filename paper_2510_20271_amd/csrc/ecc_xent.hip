@@ -15,8 +15,8 @@
 
 namespace ecc {
 
-// float16 (a type of its own, or float32's planes) holds dz as a multiple of 2^-14 of the largest upstream gradient: the probabilities
-// of a large vocabulary are far below its least number otherwise.  (They are at most 1: 2^14 is in range.  Values are good to 2^-39 of
+// float16 holds dz as a multiple of 2^-14 of the largest upstream gradient: the probabilities of a large vocabulary are far below its
+// least number otherwise.  (They are at most 1: 2^14 is in range.  Values are good to 2^-39 of
 // the largest.)
 constexpr float kHalfScale = 16384.0f;
 
@@ -24,7 +24,7 @@ static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 static int64_t up_to(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 
 // ---- operands --------------------------------------------------------------------------------------------------------------
-// One operand to be laid out as the products take them: [planes][rows][ld], zeros behind a row's end.  blocks: 0 where the
+// One operand to be laid out as the products take them: [rows][ld], zeros behind a row's end.  blocks: 0 where the
 // caller's own memory will do.
 struct Lay {
   const void* from;
@@ -34,24 +34,6 @@ struct Lay {
 // A thread lays out chunks of 8 elements: of row `row` from element k.  Rows start anywhere, so whole chunks are fetched at the
 // alignment of an element (8 fetches of an element each: 72 us for 125 MB of float32, 47 so).
 constexpr int kLayTurns = 4;
-template <typename GO>
-__device__ __forceinline__ void lay_turns(const Lay& l, int ld, int64_t block, GO&& go) {
-  const int64_t all = l.rows * ld, at = (block * kLayTurns * 256 + threadIdx.x) * 8;
-  const int hop = 256 * 8 / ld, move = 256 * 8 - hop * ld;  // rows and elements from one turn to the next
-  int64_t row = at / ld;
-  int k = (int)(at - row * ld);
-#pragma unroll
-  for (int t = 0; t < kLayTurns; ++t) {
-    if (at + t * 256 * 8 >= all) return;
-    go(row, k, at + t * 256 * 8);
-    row += hop;
-    k += move;
-    if (k >= ld) {
-      k -= ld;
-      ++row;
-    }
-  }
-}
 template <typename T>
 struct Eight { T e[8]; };
 template <typename T>
@@ -69,147 +51,23 @@ __device__ __forceinline__ Eight<T> eight_of(const Lay& l, int dim, int64_t row,
 template <typename T>
 __device__ __forceinline__ void lay_chunks(const Lay& l, int dim, int ld, int64_t block) {
   using Bits = typename std::conditional<sizeof(T) == 4, unsigned, unsigned short>::type;
-  lay_turns(l, ld, block, [&](int64_t row, int k, int64_t at) {
+  const int64_t all = l.rows * ld, at = (block * kLayTurns * 256 + threadIdx.x) * 8;
+  const int hop = 256 * 8 / ld, move = 256 * 8 - hop * ld;  // rows and elements from one turn to the next
+  int64_t row = at / ld;
+  int k = (int)(at - row * ld);
+#pragma unroll
+  for (int t = 0; t < kLayTurns; ++t) {
+    const int64_t here = at + t * 256 * 8;
+    if (here >= all) return;
     const Eight<Bits> w = eight_of<Bits>(l, dim, row, k);
-    __builtin_memcpy(__builtin_assume_aligned(static_cast<Bits*>(l.to) + at, 16), &w, sizeof(w));
-  });
-}
-
-// ---- float32 as planes of float16 --------------------------------------------------------------------------------------------
-// The largest finite |value| of each operand, and whether any is NaN or Inf: a partial result a block.
-constexpr int kRangeBlocks = 1024;  // of each operand, at most
-struct Range { float most, wild; };
-__device__ __forceinline__ Range block_range(Range r, Range (&room)[4]) {  // of 256 threads
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    r.most = fmaxf(r.most, __shfl_xor(r.most, o));
-    r.wild = fmaxf(r.wild, __shfl_xor(r.wild, o));
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = r;
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    r.most = fmaxf(r.most, room[k].most);
-    r.wild = fmaxf(r.wild, room[k].wild);
-  }
-  return r;
-}
-// (rows that are left out count for nothing here too, whatever they hold)
-template <bool ROWS>
-__device__ __forceinline__ Range range_of(const XentArgs& a, const float* p, int64_t n, int64_t i, int64_t step) {
-  Range r{0.0f, 0.0f};
-  const auto add = [&](float x) {
-    const float v = fabsf(x);
-    if (v < INFINITY) r.most = fmaxf(r.most, v);
-    else r.wild = 1.0f;
-  };
-  const int64_t quads = reinterpret_cast<uintptr_t>(p) % 16 == 0 ? n / 4 : 0;
-  const float4* q = reinterpret_cast<const float4*>(p);
-  if (!ROWS) {
-#pragma unroll 4
-    for (int64_t k = i; k < quads; k += step) {
-      const float4 x = q[k];
-      add(x.x); add(x.y); add(x.z); add(x.w);
-    }
-    for (int64_t k = quads * 4 + i; k < n; k += step) add(p[k]);
-    return r;
-  }
-  // (the row and column of a thread's values move on by the same amount every turn: no division in the loop)
-  const int size = quads ? 4 : 1;
-  const int64_t hop = step * size / a.dim;
-  const int move = (int)(step * size - hop * a.dim);
-  int64_t row = i * size / a.dim;
-  int col = (int)(i * size - row * a.dim);
-#pragma unroll 4
-  for (int64_t k = i; k < (quads ? quads : n); k += step) {
-    if (size == 1) {
-      if (a.labels[row] != a.ignore) add(p[k]);
-    } else {
-      const float4 x = q[k];
-      const float v[4] = {x.x, x.y, x.z, x.w};
-      if (col + 4 <= a.dim) {
-        if (a.labels[row] != a.ignore) {
-          add(v[0]); add(v[1]); add(v[2]); add(v[3]);
-        }
-      } else {  // over a row's end
-        for (int e = 0; e < 4; ++e)
-          if (a.labels[row + (col + e) / a.dim] != a.ignore) add(v[e]);
-      }
-    }
+    __builtin_memcpy(__builtin_assume_aligned(static_cast<Bits*>(l.to) + here, 16), &w, sizeof(w));
     row += hop;
-    col += move;
-    if (col >= a.dim) {
-      col -= a.dim;
+    k += move;
+    if (k >= ld) {
+      k -= ld;
       ++row;
     }
   }
-  for (int64_t k = quads * 4 + i; quads && k < n; k += step)
-    if (a.labels[k / a.dim] != a.ignore) add(p[k]);
-  return r;
-}
-__global__ __launch_bounds__(256) void xent_range_kernel(XentArgs a, int blocks_h, Range* part) {
-  __shared__ Range room[4];
-  const int b = (int)blockIdx.x, blocks_w = (int)gridDim.x - blocks_h;
-  const bool of_h = b < blocks_h;
-  const int at = of_h ? b : b - blocks_h;
-  const int64_t i = (int64_t)at * 256 + threadIdx.x;
-  Range r = of_h ? range_of<true>(a, static_cast<const float*>(a.h), a.rows * a.dim, i, (int64_t)blocks_h * 256)
-                 : range_of<false>(a, static_cast<const float*>(a.w), a.classes * a.dim, i, (int64_t)blocks_w * 256);
-  r = block_range(r, room);
-  if (threadIdx.x == 0) part[(of_h ? 0 : kRangeBlocks) + at] = r;
-}
-// the exponents of what the operands' values are multiplied by, from the partials; wild: a NaN or Inf in either
-struct Planes { int h, w; bool wild; };
-__device__ __forceinline__ int exponent_of(float most) {
-  return most > 0.0f ? 14 - max((int)(__float_as_uint(most) >> 23) - 127, -100) : 14;
-}
-__device__ __forceinline__ Planes planes_of(const Range* part, int blocks_h, int blocks_w, Range (&room)[4]) {
-  const auto join = [&](const Range* p, int blocks) {
-    Range r{0.0f, 0.0f};
-    for (int t = (int)threadIdx.x; t < blocks; t += 256) {
-      r.most = fmaxf(r.most, p[t].most);
-      r.wild = fmaxf(r.wild, p[t].wild);
-    }
-    return block_range(r, room);
-  };
-  const Range h = join(part, blocks_h), w = join(part + kRangeBlocks, blocks_w);
-  return {exponent_of(h.most), exponent_of(w.most), h.wild + w.wild > 0.0f};
-}
-// x s as two float16 values that add up to it.  Where the operands hold a NaN or Inf (wild) both are cut off instead of rounded, so
-// that they have x's sign, and none of a value that is not 0 is: Inf then meets no zero in the three products that its own product
-// does not.
-__device__ __forceinline__ void split2(float x, bool wild, half_t& high, half_t& low) {
-  if (!wild) {
-    high = (half_t)x;
-    low = (half_t)(x - (float)high);
-    return;
-  }
-  if (!(fabsf(x) < INFINITY)) {
-    high = (half_t)x;
-    low = x != x ? (half_t)0.0f : __builtin_bit_cast(half_t, (unsigned short)(x < 0.0f ? 0x8001 : 0x0001));
-    return;
-  }
-  const half_t least = __builtin_bit_cast(half_t, (unsigned short)(x < 0.0f ? 0x8001 : 0x0001));
-  high = __builtin_bit_cast(half_t, (unsigned short)(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(x, 0.0f)) & 0xffffu));
-  const float rest = x - (float)high;
-  low = __builtin_bit_cast(half_t, (unsigned short)(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(rest, 0.0f)) & 0xffffu));
-  if (x != 0.0f) {
-    if ((float)high == 0.0f) high = least;
-    if ((float)low == 0.0f) low = least;
-  }
-}
-__device__ __forceinline__ void lay_planes(const Lay& l, int dim, int ld, int64_t block, int exponent, bool wild) {
-  const float by = ldexpf(1.0f, exponent);
-  const int64_t all = l.rows * ld;
-  lay_turns(l, ld, block, [&](int64_t row, int k, int64_t at) {
-    const Eight<float> x = eight_of<float>(l, dim, row, k);
-    Eight<half_t> high, low;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) split2(x.e[i] * by, wild, high.e[i], low.e[i]);
-    __builtin_memcpy(__builtin_assume_aligned(static_cast<half_t*>(l.to) + at, 16), &high, 16);
-    __builtin_memcpy(__builtin_assume_aligned(static_cast<half_t*>(l.to) + all + at, 16), &low, 16);
-  });
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------
@@ -267,20 +125,18 @@ __global__ __launch_bounds__(1024) void xent_long_row_kernel(XentArgs a, const f
 }
 
 // Logits whose sums were split (few tiles, long rows of features): a row's maximum and sum, as a tile's epilogue leaves them ...
-__global__ __launch_bounds__(256) void xent_fold_kernel(XentArgs a, const float* sums, int splits, const float* unscale,
-                                                        float2* part, float* picked, int team) {
+__global__ __launch_bounds__(256) void xent_fold_kernel(XentArgs a, const float* sums, int splits, float2* part, float* picked,
+                                                        int team) {
   const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / team;
   const int lane = threadIdx.x & (team - 1);
   const bool in = row < a.rows;
   const int64_t all = a.rows * a.classes, label = in ? a.labels[row] : -1;
   const float* z = sums + (in ? row : 0) * a.classes;
-  const float by = unscale ? unscale[0] : 1.0f, by2 = unscale ? unscale[1] : 1.0f;
   float m = -INFINITY, s = 0.0f;
   for (int64_t v = lane; v < a.classes; v += team) {
     float x = 0.0f;
 #pragma unroll 4
     for (int k = 0; k < splits; ++k) x += z[k * all + v];
-    x = x * by * by2;
     if (in && v == label) picked[row] = x;
     const float top = fmaxf(m, x), base = top == -INFINITY ? 0.0f : top;
     s = s * __expf(m - base) + (v == label ? 0.0f : __expf(x - base));
@@ -294,25 +150,23 @@ __global__ __launch_bounds__(256) void xent_fold_kernel(XentArgs a, const float*
   if (in && lane == 0) part[row] = make_float2(m, s);
 }
 // ... or their gradient, [planes][rows][ld], for `count` classes from v0
-template <typename E, int PLANES>
+template <typename T>
 __global__ __launch_bounds__(256) void xent_dz_kernel(XentArgs a, const float* sums, int splits, int64_t v0, int64_t count, int64_t ld,
-                                                      const float* row_scale, const float* unscale, E* dz) {
+                                                      const float* row_scale, T* dz) {
   const int64_t all = a.rows * ld, n = a.rows * count;
-  const float by = unscale ? unscale[0] : 1.0f, by2 = unscale ? unscale[1] : 1.0f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / ld, v = i - row * ld, label = a.labels[row];
     float f = 0.0f;
     if (v < count && label != a.ignore) {
       float x = sums[row * count + v];
       for (int k = 1; k < splits; ++k) x += sums[k * n + row * count + v];
-      x = x * by * by2;
       const double lse = a.stats[row * 2];
       const float high = (float)lse, low = (float)(lse - (double)high);
       f = (v0 + v == label ? -(float)a.stats[row * 2 + 1] : __expf((x - high) - low)) * row_scale[row];
     }
 #pragma unroll
-    for (int k = 0; k < planes_of_dz(PLANES); ++k) {
-      const E e = narrow<E>(f);
+    for (int k = 0; k < kPlanes<T>; ++k) {
+      const T e = narrow<T>(f);
       dz[k * all + i] = e;
       f -= widen(e);
     }
@@ -427,21 +281,15 @@ __global__ __launch_bounds__(kSumThreads) void xent_top_kernel(XentArgs a, float
 
 // What each row's dz is multiplied by, which rows count, and what the products are multiplied by.
 struct Scales {
-  const float* top;  // float16 planes with a gradient for each row: the largest of them
-  float* row_scale;  // null: forward
+  const float* top;  // float16 with a gradient for each row: the largest of them
+  float* row_scale;
   unsigned long long* keep;
-  float* scale;      // [4]: of the gradient of hidden, of the weight's, of logits (two factors: one could overflow)
+  float* scale;      // [1]: of both gradients
   bool half;         // dz is held in float16
   int64_t blocks;    // 0: none wanted
 };
-__device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, int64_t block, int exponent_h, int exponent_w) {
+__device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, int64_t block) {
   const int64_t i = block * 256 + threadIdx.x;
-  if (i == 0) {
-    const int exponent = -exponent_h - exponent_w;
-    c.scale[2] = ldexpf(1.0f, exponent / 2);
-    c.scale[3] = ldexpf(1.0f, exponent - exponent / 2);
-  }
-  if (!c.row_scale) return;
   float by = c.half ? kHalfScale : 1.0f, back = 1.0f / by;
   if (a.reduction == kEach) {
     if (c.half) {
@@ -463,10 +311,7 @@ __device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, i
   }
   const unsigned long long bits = __ballot(counts);
   if ((threadIdx.x & 63) == 0 && i < a.rows) c.keep[i / 64] = bits;
-  if (i == 0) {
-    c.scale[0] = (float)((double)back * ldexp(1.0, -exponent_w));
-    c.scale[1] = (float)((double)back * ldexp(1.0, -exponent_h));
-  }
+  if (i == 0) c.scale[0] = back;
 }
 
 // What comes before the products, in one launch: both operands laid out and the rows' scales, a run of blocks each.
@@ -476,18 +321,7 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(XentArgs a, Lay h, La
   if (block < h.blocks) return lay_chunks<T>(h, a.dim, ld, block);
   block -= h.blocks;
   if (block < w.blocks) return lay_chunks<T>(w, a.dim, ld, block);
-  scale_rows(a, c, block - w.blocks, 0, 0);
-}
-__global__ __launch_bounds__(256) void xent_prepare_planes_kernel(XentArgs a, Lay h, Lay w, int ld, Scales c, const Range* part,
-                                                                  int blocks_h, int blocks_w) {
-  __shared__ Range room[4];
-  int64_t block = blockIdx.x;
-  Planes p{0, 0, false};
-  if (block <= h.blocks + w.blocks) p = planes_of(part, blocks_h, blocks_w, room);  // (the first behind the operands writes the scales)
-  if (block < h.blocks) return lay_planes(h, a.dim, ld, block, p.h, p.wild);
-  block -= h.blocks;
-  if (block < w.blocks) return lay_planes(w, a.dim, ld, block, p.w, p.wild);
-  scale_rows(a, c, block - w.blocks, p.h, p.w);
+  scale_rows(a, c, block - w.blocks);
 }
 
 // out = narrow(scale * sum of the splits), `team` threads to an element, added in a fixed order
@@ -518,42 +352,32 @@ __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int sp
 }
 
 // ---- plans -----------------------------------------------------------------------------------------------------------------
-constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of a plane of dz, and of laid-out weights: what the Infinity Cache holds
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of two bytes of every dz (a plane of it), and of laid-out weights
 constexpr int64_t kPieceFew = (int64_t)1 << 30;      // of laid-out weights where rows are few
 constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
 constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 
-// float32: by the float32 instruction where rows or classes are a tile or fewer, where the operands' way from memory counts (steps: 128
-// rows x 2364 x 31381 753 us so, 939 by planes; 200 rows, a second tile, 1229 so, 1039 by planes; 100000 x 512 x 100 545 so, 573 by
-// planes), and where the whole is so small that two launches more count (502 x 102 x 18, the loss alone: 20 us so, 24 by planes; 400 x
-// 511 x 2000, step: 216 so, 182 by planes); by planes of float16 otherwise.  16-bit: two planes of dz.
-static bool few_rows(int64_t rows, int64_t dim, int64_t classes, int dtype) {
-  if (dtype != kF32) return false;
-  return rows <= 128 || classes <= 128 || rows * dim <= ((int64_t)1 << 28) / classes;
-}
-static int way_of(int64_t rows, int64_t dim, int64_t classes, int dtype) {
-  const bool few = few_rows(rows, dim, classes, dtype);
-  return dtype == kF32 ? (few ? kOne : kBoth) : kTwo;
-}
 static int ld_of(int dim) { return (int)up_to(dim, 8); }
 
-// Tiles of 256 x 256 where they fill the card (one block a CU) and the summed axis is eight turns or more; of 128 x 128
+// Tiles of 256 x 256 (`large`) where they fill the card (one block a CU) and the summed axis is eight turns or more; of 128 x 128
 // otherwise, two blocks a CU, so that one's start and end run beside the other's products.  Thin products have thin tiles.
-// (385475 x 18 x 599 in float16, one turn: logits 228 us by large tiles, 176 by the others.)
-static int shape_of(int64_t M, int64_t N, int64_t runs, int64_t turns, bool few = false) {
+// (385475 x 18 x 599 in float16, one turn: logits 228 us by large tiles, 176 by the others.)  float32 logits by the smaller ones: a
+// round of tiles is four times as long there as a 16-bit one, and the last one is seldom full (4096 x 512 x 10007: 383 us, 436 by
+// large tiles; gradients, whose sums are split into whole rounds: of the weight 385 by large ones, 553).
+static int shape_of(int64_t M, int64_t N, int64_t runs, int64_t turns, bool large) {
   if (N <= 32) return 2;
   if (M <= 32) return 3;
   if (N <= 64) return 5;
   if (M <= 64 && N > 128) return 4;
-  const int64_t large = (M + 255) / 256 * ((N + 255) / 256);
-  return !few && M > 128 && N > 128 && turns >= 8 && large * runs >= 256 ? 0 : 1;
+  const int64_t tiles = (M + 255) / 256 * ((N + 255) / 256);
+  return large && M > 128 && N > 128 && turns >= 8 && tiles * runs >= 256 ? 0 : 1;
 }
 // The summed axis in runs, so that blocks fill the card: eight turns a run or more, results within kSumsBytes.
-static int splits_of(int64_t M, int64_t N, int64_t K, int shape, int pairs, int depth) {
+static int splits_of(int64_t M, int64_t N, int64_t K, int shape, int planes, int depth) {
   const ProductPlan& p = kPlans[shape];
   const int64_t blocks = (M + p.bm - 1) / p.bm * ((N + p.bn - 1) / p.bn), total = (K + depth - 1) / depth;
   const int64_t fill = shape == 0 ? 256 : 512;  // blocks that the card holds
-  int64_t want = std::min(std::max<int64_t>(1, fill / blocks), std::max<int64_t>(1, total * pairs / 8));
+  int64_t want = std::min(std::max<int64_t>(1, fill / blocks), std::max<int64_t>(1, total * planes / 8));
   want = std::max<int64_t>(1, std::min({want, total, kSumsBytes / (M * N * 4)}));
   const int64_t steps = (total + want - 1) / want;
   return (int)((total + steps - 1) / steps);
@@ -565,16 +389,14 @@ struct XentPlan {
   int64_t parts;
   bool hidden_sums;
   size_t lay_h, lay_w, lay_w_fwd;                        // bytes of laid-out operands
-  size_t range, scalars;                                 // planes' ranges, scales
   size_t part, picked, each, row_sums, sums_f;           // forward
-  size_t dz, sums_z, sums_h, sums_w, row_scale, keep;    // backward
+  size_t dz, sums_z, sums_h, sums_w, row_scale, keep, scalars;  // backward
 };
 
 static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   XentPlan p{};
-  const int way = way_of(rows, dim, classes, dtype), P = way == kBoth ? 2 : 1, Z = planes_of_dz(way);
-  const bool few = few_rows(rows, dim, classes, dtype);
-  const int64_t size = dtype == kF32 && few ? 4 : 2;  // of a plane's element
+  const int64_t size = dtype == kF32 ? 4 : 2;
+  const int planes = dtype == kF32 ? kPlanes<float> : kPlanes<half_t>, depth = 128 / (int)size;
   const int64_t ld = ld_of(dim);
   // Pieces of at most `most` classes, equal ones.  Where the last piece is small anyway the others hold whole rounds of 256 large
   // tiles (2048 rows, 50021 classes: 32768 and 17253, 4 + 3 rounds of blocks; halves: 4 + 4).
@@ -586,54 +408,52 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
     if (most / round * round * count >= classes) return most / round * round;
     return up_to((classes + count - 1) / count, 256);
   };
-  const int pairs = way == kBoth ? 3 : 1, pairs_z = way, depth = 128 / (int)size;
-  const int64_t dim_turns = (dim + depth - 1) / depth * pairs;
-  p.fwd_shape = shape_of(classes, rows, 1, dim_turns, few);
+  const int64_t dim_turns = (dim + depth - 1) / depth;
+  p.fwd_shape = shape_of(classes, rows, 1, dim_turns, size == 2);
   p.parts = (classes + kPlans[p.fwd_shape].bm - 1) / kPlans[p.fwd_shape].bm * kPlans[p.fwd_shape].wm;
   // (few rows: pieces of as many tiles as the card holds blocks, within kPieceFew; 38 x 2030 x 92507 in float32: products 485 us by
   // pieces of kPieceBytes, 266 so)
   const int64_t tiles = (rows + kPlans[p.fwd_shape].bn - 1) / kPlans[p.fwd_shape].bn;
   const int64_t full = std::min((512 + tiles - 1) / tiles * kPlans[p.fwd_shape].bm, kPieceFew / (ld * size));
   p.fwd_piece = pieces(std::min(kPieceMost * 8, std::max(full, kPieceBytes / (ld * size))));
-  p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * size), way == kBoth ? kPieceBytes / (ld * size) : kPieceMost}));
+  p.piece = pieces(std::min(kPieceMost, kPieceBytes / (rows * 2)));
   p.ld_dz = up_to(p.piece, 8);
-  p.shape = shape_of(p.piece, rows, 1, dim_turns, few);
+  p.shape = shape_of(p.piece, rows, 1, dim_turns, size == 2);
   // logits by split sums: where their tiles leave compute units idle through a long sum
   const auto split = [&](int64_t M, int shape) {
-    const int splits = dim_turns < 16 || M > 1024 ? 1 : splits_of(M, rows, dim, shape, pairs, depth);
+    const int splits = dim_turns < 16 || M > 1024 ? 1 : splits_of(M, rows, dim, shape, 1, depth);
     return splits >= 4 ? splits : 1;
   };
   p.fwd_splits = classes <= p.fwd_piece ? split(classes, p.fwd_shape) : 1;
   p.splits = split(p.piece, p.shape);
   if (p.fwd_splits > 1) p.parts = 1;
   const int64_t long_k = std::max<int64_t>(1, p.piece / depth / 16), long_n = std::max<int64_t>(1, rows / depth / 16);
-  p.hidden_shape = shape_of(dim, rows, long_k, p.piece / depth * pairs_z, few);
-  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape, pairs_z, depth);
+  p.hidden_shape = shape_of(dim, rows, long_k, p.piece / depth * planes, true);
+  p.hidden_splits = splits_of(dim, rows, p.piece, p.hidden_shape, planes, depth);
   p.hidden_sums = p.hidden_splits > 1 || p.piece < classes;
-  p.weight_shape = shape_of(dim, p.piece, long_n, rows / depth * pairs_z, few);
-  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, pairs_z, depth);
-  p.lay_h = align256((size_t)rows * ld * size * P);
-  p.lay_w = align256((size_t)p.piece * ld * size * P);
-  p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * size * P);
+  p.weight_shape = shape_of(dim, p.piece, long_n, rows / depth * planes, true);
+  p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, planes, depth);
+  p.lay_h = align256((size_t)rows * ld * size);
+  p.lay_w = align256((size_t)p.piece * ld * size);
+  p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * size);
   p.part = align256((size_t)rows * p.parts * sizeof(float2));
   p.picked = p.each = align256((size_t)rows * 4);
   p.row_sums = align256(256 * sizeof(RowSum));
   p.sums_f = p.fwd_splits > 1 ? align256((size_t)p.fwd_splits * rows * classes * 4) : 0;
   p.sums_z = p.splits > 1 ? align256((size_t)p.splits * rows * p.piece * 4) : 0;
-  p.dz = align256((size_t)rows * p.ld_dz * size * Z);
+  p.dz = align256((size_t)rows * p.ld_dz * size * planes);
   p.sums_h = p.hidden_sums ? align256((size_t)p.hidden_splits * rows * dim * 4) : 0;
   p.sums_w = p.weight_splits > 1 ? align256((size_t)p.weight_splits * p.piece * dim * 4) : 0;
   p.row_scale = align256((size_t)rows * 4);
   p.keep = align256((size_t)(rows + 63) / 64 * 8);
   p.scalars = 256;
-  p.range = align256(2 * kRangeBlocks * sizeof(Range));
   return p;
 }
 
 size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int dtype, bool backward) {
   const XentPlan p = xent_plan(rows, dim, classes, dtype);
-  if (!backward) return p.lay_h + p.lay_w_fwd + p.part + p.picked + p.each + p.row_sums + p.sums_f + p.range + p.scalars;
-  return p.lay_h + p.lay_w + p.dz + p.sums_z + p.sums_h + p.sums_w + p.row_scale + p.keep + p.range + p.scalars;
+  if (!backward) return p.lay_h + p.lay_w_fwd + p.part + p.picked + p.each + p.row_sums + p.sums_f;
+  return p.lay_h + p.lay_w + p.dz + p.sums_z + p.sums_h + p.sums_w + p.row_scale + p.keep + p.scalars;
 }
 
 struct Room {  // hands out a workspace
@@ -647,8 +467,7 @@ struct Room {  // hands out a workspace
 
 // Whether the products can read the caller's own memory: whole elements, rows of whole 16-byte chunks.
 static bool as_it_is(const XentArgs& a, const void* p, int dtype) {
-  const int dim = a.dim;
-  return way_of(a.rows, dim, a.classes, dtype) != kBoth && dim % (dtype == kF32 ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+  return a.dim % (dtype == kF32 ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
 // An operand as the products see it, and what has to be laid out for that.
@@ -658,24 +477,13 @@ static Matrix laid(const void* from, int64_t rows, int dim, void* room, bool own
   if (own) return {from, rows, dim, 0};
   return {room, rows, ld, rows * ld};
 }
-// blocks that look for an operand's range: 16 values a thread or more
-static int range_blocks(int64_t n) { return (int)std::max<int64_t>(1, std::min<int64_t>(kRangeBlocks, n / 4096)); }
-template <typename T, int PLANES>
-static void prepare(const XentArgs& a, const Lay& h, const Lay& w, const Scales& c, Range* range, hipStream_t st) {
-  if constexpr (PLANES == kBoth) {
-    const int bh = range_blocks(a.rows * a.dim), bw = range_blocks(a.classes * a.dim);
-    if (c.blocks)  // (the first piece)
-      hipLaunchKernelGGL(xent_range_kernel, dim3((unsigned)(bh + bw)), dim3(256), 0, st, a, bh, range);
-    hipLaunchKernelGGL(xent_prepare_planes_kernel, dim3((unsigned)(h.blocks + w.blocks + c.blocks)), dim3(256), 0, st, a, h, w,
-                       ld_of(a.dim), c, range, bh, bw);
-  } else {
-    const int64_t blocks = h.blocks + w.blocks + c.blocks;
-    if (blocks) hipLaunchKernelGGL(xent_prepare_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, a, h, w, ld_of(a.dim), c);
-  }
+template <typename T>
+static void prepare(const XentArgs& a, const Lay& h, const Lay& w, const Scales& c, hipStream_t st) {
+  const int64_t blocks = h.blocks + w.blocks + c.blocks;
+  if (blocks) hipLaunchKernelGGL(xent_prepare_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, a, h, w, ld_of(a.dim), c);
 }
 
-// T: element type of the arguments, E: of the products' operands
-template <typename T, typename E, int PLANES>
+template <typename T>
 static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
   Room room{static_cast<char*>(a.ws)};
@@ -685,10 +493,6 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   float* each = static_cast<float*>(room.take(p.each));
   RowSum* row_sums = static_cast<RowSum*>(room.take(p.row_sums));
   float* sums = static_cast<float*>(room.take(p.sums_f));
-  Range* range = static_cast<Range*>(room.take(p.range));
-  float* scale = static_cast<float*>(room.take(p.scalars));
-  Scales scales{nullptr, nullptr, nullptr, scale, false, PLANES == kBoth ? 1 : 0};
-  const float* unscale = PLANES == kBoth ? scale + 2 : nullptr;
   if (a.reduction == kEach) each = a.loss;
   const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
   ProductArgs g{};
@@ -702,7 +506,6 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   g.part = part;
   g.parts = p.parts;
   g.picked = picked;
-  g.unscale = unscale;
   const bool own = as_it_is(a, w, dtype);
   const ProductPlan& plan = kPlans[p.fwd_shape];
   // (all classes at once where nothing is laid out, but no more blocks than a grid may have)
@@ -712,19 +515,19 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   for (int64_t v0 = 0; v0 < a.classes && e == hipSuccess; v0 += piece) {
     const int64_t count = std::min(piece, a.classes - v0);
     g.a = laid(w + v0 * a.dim, count, a.dim, lay_w, own, &lw);
-    prepare<T, PLANES>(a, lh, lw, scales, range, st);
-    lh.blocks = scales.blocks = 0;
+    prepare<T>(a, lh, lw, Scales{}, st);
+    lh.blocks = 0;
     g.M = count;
     g.v0 = v0;
     g.part0 = v0 / plan.bm * plan.wm;
-    e = launch_product<E, T, PLANES>(kLogits, p.fwd_splits > 1 ? kSums : kForward, p.fwd_shape, g, st);
+    e = launch_product<T>(kLogits, p.fwd_splits > 1 ? kSums : kForward, p.fwd_shape, g, st);
   }
   if (e != hipSuccess) return e;
   int team = 64;
   if (p.fwd_splits > 1) {
     while (team > 1 && team / 2 >= a.classes) team /= 2;
     hipLaunchKernelGGL(xent_fold_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, sums, p.fwd_splits,
-                       unscale, part, picked, team);
+                       part, picked, team);
     team = 64;
   }
   while (team > 1 && team / 2 >= p.parts) team /= 2;
@@ -756,7 +559,7 @@ static void xent_out(const float* sums, int splits, int64_t n, const float* scal
   hipLaunchKernelGGL(xent_out_kernel<T>, dim3(blocks), dim3(256), 0, st, sums, splits, n, scale, team, out);
 }
 
-template <typename T, typename E, int PLANES>
+template <typename T>
 static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
   Room room{static_cast<char*>(a.ws)};
@@ -766,14 +569,12 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   float* sums_w = static_cast<float*>(room.take(p.sums_w));
   float* row_scale = static_cast<float*>(room.take(p.row_scale));
   unsigned long long* keep = static_cast<unsigned long long*>(room.take(p.keep));
-  Range* range = static_cast<Range*>(room.take(p.range));
   float* scale = static_cast<float*>(room.take(p.scalars));
   const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
-  const bool half = dtype == kF16 || PLANES == kBoth;
-  const float* unscale = PLANES == kBoth ? scale + 2 : nullptr;
+  const bool half = dtype == kF16;
   if (half && a.reduction == kEach)
-    hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a, scale + 4);
-  Scales scales{scale + 4, row_scale, keep, scale, half, (a.rows + 255) / 256};
+    hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a, scale + 1);
+  Scales scales{scale + 1, row_scale, keep, scale, half, (a.rows + 255) / 256};
   Lay lh, lw;
   const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(a, h, dtype), &lh);
   const bool own = as_it_is(a, w, dtype);
@@ -781,31 +582,29 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   for (int64_t v0 = 0; v0 < a.classes; v0 += p.piece) {
     const int64_t count = std::min(p.piece, a.classes - v0), ld = up_to(count, 8);
     const Matrix wm = laid(w + v0 * a.dim, count, a.dim, lay_w, own, &lw);
-    prepare<T, PLANES>(a, lh, lw, scales, range, st);
+    prepare<T>(a, lh, lw, scales, st);
     lh.blocks = scales.blocks = 0;
     const Matrix zm{dz, a.rows, ld, a.rows * ld};
     ProductArgs g{};
-    g.unscale = unscale;
     // dz of the piece
     g.a = wm; g.b = hm; g.M = count; g.N = a.rows; g.K = a.dim; g.splits = p.splits; g.sums = sums_z; g.add = 0;
     g.labels = a.labels; g.ignore = a.ignore; g.v0 = v0; g.stats = a.stats; g.row_scale = row_scale;
     g.dz = dz; g.dz_ld = ld; g.dz_plane = a.rows * ld;
-    e = p.splits > 1 ? launch_product<E, T, PLANES == kTwo ? kOne : PLANES>(kLogits, kSums, p.shape, g, st)
-                     : launch_product<E, T, PLANES>(kLogits, kBackward, p.shape, g, st);
+    e = launch_product<T>(kLogits, p.splits > 1 ? kSums : kBackward, p.shape, g, st);
     if (e != hipSuccess) return e;
     if (p.splits > 1) {
       const unsigned blocks = (unsigned)std::min<int64_t>((a.rows * ld + 255) / 256, 4096);
-      hipLaunchKernelGGL((xent_dz_kernel<E, PLANES>), dim3(blocks), dim3(256), 0, st, a, sums_z, p.splits, v0, count, ld, row_scale,
-                         unscale, static_cast<E*>(dz));
+      hipLaunchKernelGGL(xent_dz_kernel<T>, dim3(blocks), dim3(256), 0, st, a, sums_z, p.splits, v0, count, ld, row_scale,
+                         static_cast<T*>(dz));
     }
     if (a.dh) {
       g.a = wm; g.b = zm; g.M = a.dim; g.N = a.rows; g.K = count;
-      g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape, PLANES, 128 / (int)sizeof(E)));
+      g.splits = std::min(p.hidden_splits, splits_of(a.dim, a.rows, count, p.hidden_shape, kPlanes<T>, kDepth<T>));
       g.sums = p.hidden_sums ? sums_h : nullptr;
       g.add = v0 > 0;
       g.out = a.dh;
       g.scale = scale;
-      if ((e = launch_product<E, T, PLANES>(kHidden, 0, p.hidden_shape, g, st)) != hipSuccess) return e;
+      if ((e = launch_product<T>(kHidden, 0, p.hidden_shape, g, st)) != hipSuccess) return e;
     }
     if (a.dw) {
       T* out = static_cast<T*>(a.dw) + v0 * a.dim;
@@ -814,22 +613,20 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
       g.sums = p.weight_splits > 1 ? sums_w : nullptr;
       g.add = 0;
       g.out = out;
-      g.scale = scale + 1;
-      if ((e = launch_product<E, T, PLANES>(kWeight, 0, p.weight_shape, g, st)) != hipSuccess) return e;
-      if (g.sums) xent_out(sums_w, p.weight_splits, count * a.dim, scale + 1, out, st);
+      g.scale = scale;
+      if ((e = launch_product<T>(kWeight, 0, p.weight_shape, g, st)) != hipSuccess) return e;
+      if (g.sums) xent_out(sums_w, p.weight_splits, count * a.dim, scale, out, st);
     }
   }
   if (a.dh && p.hidden_sums) xent_out(sums_h, p.hidden_splits, a.rows * a.dim, scale, static_cast<T*>(a.dh), st);
   return hipGetLastError();
 }
 
-#define ECC_GO(WAY, PLANES)                                                                                               \
-  if (dtype == kF32)                                                                                                       \
-    return few_rows(a.rows, a.dim, a.classes, dtype) ? WAY<float, float, kOne>(a, dtype, st)                               \
-                                                     : WAY<float, half_t, kBoth>(a, dtype, st);                            \
-  return dtype == kF16 ? WAY<half_t, half_t, PLANES>(a, dtype, st) : WAY<bf16_t, bf16_t, PLANES>(a, dtype, st)
-hipError_t launch_xent_fwd(const XentArgs& a, int dtype, hipStream_t st) { ECC_GO(xent_fwd, kOne); }
-hipError_t launch_xent_bwd(const XentArgs& a, int dtype, hipStream_t st) { ECC_GO(xent_bwd, kTwo); }
-#undef ECC_GO
+hipError_t launch_xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
+  return dtype == kF32 ? xent_fwd<float>(a, dtype, st) : dtype == kF16 ? xent_fwd<half_t>(a, dtype, st) : xent_fwd<bf16_t>(a, dtype, st);
+}
+hipError_t launch_xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
+  return dtype == kF32 ? xent_bwd<float>(a, dtype, st) : dtype == kF16 ? xent_bwd<half_t>(a, dtype, st) : xent_bwd<bf16_t>(a, dtype, st);
+}
 
 }  // namespace ecc

@@ -2,5 +2,5 @@
 #include "ecc_xent_launch.h"
 
 namespace ecc {
-template hipError_t launch_product<half_t, half_t, kOne>(int, int, int, ProductArgs, hipStream_t);
+template hipError_t launch_product<half_t>(int, int, int, ProductArgs, hipStream_t);
 }

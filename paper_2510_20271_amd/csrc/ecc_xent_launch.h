@@ -1,4 +1,4 @@
-// Instances of the product kernels for one pair of element types (included by the ecc_xent_*.hip files).
+// Instances of the product kernels for one element type (included by the ecc_xent_*.hip files).
 #pragma once
 #include <atomic>
 
@@ -24,22 +24,20 @@ static hipError_t product_go(const ProductArgs& g, int threads, hipStream_t st) 
   return hipGetLastError();
 }
 
-template <typename T, typename O, int PLANES, int BM, int BN, int WM, int WN, int STAGES>
+template <typename T, int BM, int BN, int WM, int WN, int STAGES>
 static hipError_t product_shape(int kind, int mode, const ProductArgs& g, hipStream_t st) {
   constexpr int kShared = STAGES * (BM + BN) * 128, kThreads = WM * WN * 64;
-  if constexpr (PLANES != kTwo) {  // (forward logits and split sums know nothing of a second plane of dz)
-    if (kind == kLogits && mode == kForward)
-      return product_go<product_kernel<T, O, PLANES, kLogits, kForward, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
-    if (kind == kLogits && mode == kSums)
-      return product_go<product_kernel<T, O, PLANES, kLogits, kSums, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
-  }
-  if (kind == kLogits && mode == kBackward)
-    return product_go<product_kernel<T, O, PLANES, kLogits, kBackward, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
-  if (kind == kHidden) return product_go<product_kernel<T, O, PLANES, kHidden, 0, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
-  return product_go<product_kernel<T, O, PLANES, kWeight, 0, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kLogits && mode == kForward)
+    return product_go<product_kernel<T, kLogits, kForward, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kLogits && mode == kSums)
+    return product_go<product_kernel<T, kLogits, kSums, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kLogits)
+    return product_go<product_kernel<T, kLogits, kBackward, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  if (kind == kHidden) return product_go<product_kernel<T, kHidden, 0, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
+  return product_go<product_kernel<T, kWeight, 0, BM, BN, WM, WN, STAGES>, kShared>(g, kThreads, st);
 }
 
-template <typename T, typename O, int PLANES>
+template <typename T>
 hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStream_t st) {
   const ProductPlan& p = kPlans[shape];
   g.tiles_m = (int)((g.M + p.bm - 1) / p.bm);
@@ -47,26 +45,24 @@ hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStrea
   g.total = (int)((g.K + kDepth<T> - 1) / kDepth<T>);
   g.steps = (g.total + g.splits - 1) / g.splits;
   g.splits = (g.total + g.steps - 1) / g.steps;  // (no run is empty)
-  const int turns = g.steps * (PLANES == kBoth ? 3 : kind == kLogits ? 1 : PLANES);
+  const int turns = g.steps * (kind == kLogits ? 1 : kPlanes<T>);
   // One turn needs one tile in LDS, which leaves room for more blocks (385475 x 18 x 599 in float16: logits 176 us with two,
   // 145 with one); thin tiles are four ahead where there are turns to come (32 x 128 x 1000, 12 turns: 10.4 us with two, 7.8
   // with four).
   switch (shape) {
-    case 0:
-      if constexpr (sizeof(T) == 2) return product_shape<T, O, PLANES, 256, 256, 2, 4, 2>(kind, mode, g, st);
-      return hipErrorInvalidValue;  // (float32: not asked for)
-    case 1: return turns == 1 ? product_shape<T, O, PLANES, 128, 128, 2, 2, 1>(kind, mode, g, st)
-                              : product_shape<T, O, PLANES, 128, 128, 2, 2, 2>(kind, mode, g, st);
-    case 2: return turns == 1  ? product_shape<T, O, PLANES, 128, 32, 4, 1, 1>(kind, mode, g, st)
-                   : turns < 4 ? product_shape<T, O, PLANES, 128, 32, 4, 1, 2>(kind, mode, g, st)
-                               : product_shape<T, O, PLANES, 128, 32, 4, 1, 4>(kind, mode, g, st);
-    case 3: return turns == 1  ? product_shape<T, O, PLANES, 32, 128, 1, 4, 1>(kind, mode, g, st)
-                   : turns < 4 ? product_shape<T, O, PLANES, 32, 128, 1, 4, 2>(kind, mode, g, st)
-                               : product_shape<T, O, PLANES, 32, 128, 1, 4, 4>(kind, mode, g, st);
-    case 4: return turns == 1 ? product_shape<T, O, PLANES, 64, 256, 1, 4, 1>(kind, mode, g, st)
-                              : product_shape<T, O, PLANES, 64, 256, 1, 4, 2>(kind, mode, g, st);
-    default: return turns == 1 ? product_shape<T, O, PLANES, 128, 64, 4, 1, 1>(kind, mode, g, st)
-                               : product_shape<T, O, PLANES, 128, 64, 4, 1, 3>(kind, mode, g, st);
+    case 0: return product_shape<T, 256, 256, 2, 4, 2>(kind, mode, g, st);
+    case 1: return turns == 1 ? product_shape<T, 128, 128, 2, 2, 1>(kind, mode, g, st)
+                              : product_shape<T, 128, 128, 2, 2, 2>(kind, mode, g, st);
+    case 2: return turns == 1  ? product_shape<T, 128, 32, 4, 1, 1>(kind, mode, g, st)
+                   : turns < 4 ? product_shape<T, 128, 32, 4, 1, 2>(kind, mode, g, st)
+                               : product_shape<T, 128, 32, 4, 1, 4>(kind, mode, g, st);
+    case 3: return turns == 1  ? product_shape<T, 32, 128, 1, 4, 1>(kind, mode, g, st)
+                   : turns < 4 ? product_shape<T, 32, 128, 1, 4, 2>(kind, mode, g, st)
+                               : product_shape<T, 32, 128, 1, 4, 4>(kind, mode, g, st);
+    case 4: return turns == 1 ? product_shape<T, 64, 256, 1, 4, 1>(kind, mode, g, st)
+                              : product_shape<T, 64, 256, 1, 4, 2>(kind, mode, g, st);
+    default: return turns == 1 ? product_shape<T, 128, 64, 4, 1, 1>(kind, mode, g, st)
+                               : product_shape<T, 128, 64, 4, 1, 3>(kind, mode, g, st);
   }
 }
 

@@ -7,15 +7,12 @@
 // column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4, so a lane has a row's logits side by side (their maximum and sum need
 // no exchange but one between two lanes) and four neighbours along a result's row (stores of 8 or 16 bytes).
 //
-// Elements are 16-bit, or float32 by the float32 instruction where rows or classes are few (memory bounds those) or all is small, or
-// float32 as two float16 planes: x s = x1 + x2 with s the power of two that brings the operand's largest value to 2^14 .. 2^15, x1 the
-// nearest float16 and x2 the nearest to what is left, good to 2^-23 of x and 2^-39 of the largest.  A product is then three products
-// of planes, x1 y1 + x1 y2 + x2 y1; x2 y2, left out, is of random sign and below 2^-22 of |x| |y| (2^-25 at the middle).  Three float16
-// instructions stand against sixteen times the float32 instruction's rate.
-// 16-bit gradients dz have a second plane as well, what the first one's rounding left, so that the sums of them are off by no more than
-// float32 sums are: that rounding (2^-9 of each dz for bfloat16) is as much as the result's own, and neither sum averages it out, over
-// classes (hidden's gradient) or over rows, where one term is most of it.  It costs the two gradients' products twice the matrix
-// instructions (8192 x 4096 x 131072 bfloat16 step: 48.0 ms, 31.0 with one plane).
+// Elements are 16-bit or float32, each by the instruction of its type.  16-bit gradients dz have a second plane, what the first one's
+// rounding left, so that the sums of them are off by no more than float32 sums are: that rounding (2^-9 of each dz for bfloat16) is as
+// much as the result's own, and neither sum averages it out, over classes (hidden's gradient) or over rows, where one term is most of
+// it.  It costs the two gradients' products twice the matrix instructions (8192 x 4096 x 131072 bfloat16 step: 48.0 ms, 31.0 with one
+// plane).  float32 operands are multiplied as they are (two float16 planes of each, scaled by its largest value, stand for values down
+// to 2^-39 of that one only: 4096 x 512 x 10007 step 1366 us so, 690 by planes that lost every row beside a class masked by -1e9).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -30,7 +27,7 @@ constexpr int kBackward = 0, kForward = 1, kSums = 2;
 // elements of a tile along the summed axis: 128 bytes
 template <typename T> constexpr int kDepth = 128 / (int)sizeof(T);
 
-// A matrix [planes][rows][ld], rows of whole 16-byte chunks, 16-byte aligned; elements between a row's end and ld are 0.
+// A matrix [planes][rows][ld] (dz: kPlanes, others one), rows of whole 16-byte chunks, 16-byte aligned; elements between a row's end and ld are 0.
 struct Matrix {
   const void* p;
   int64_t rows, ld, plane;  // plane: elements from one plane to the next
@@ -49,7 +46,6 @@ struct ProductArgs {
   int add;             //   added to what is there
   void* out;           // [N][M], scaled by *scale
   const float* scale;  // [1]
-  const float* unscale;  // [2], kBoth: what logits are multiplied by
   // kLogits
   const int64_t* labels;
   int64_t v0;          // the first class of this piece (M: its classes)
@@ -77,22 +73,20 @@ using Acc = float __attribute__((ext_vector_type(16)));
 using Quad = short __attribute__((ext_vector_type(4)));
 using LdsVoid = __attribute__((address_space(3))) void;
 
-__device__ __forceinline__ Acc mma(Lanes<bf16_t>::V8 a, Lanes<bf16_t>::V8 b, Acc c) {
+// matrix instructions of a step: float32's takes two elements along the summed axis, one of each half of the lanes
+template <typename T> constexpr int kMmas = sizeof(T) == 4 ? 4 : 1;
+__device__ __forceinline__ Acc mma(Lanes<bf16_t>::V8 a, Lanes<bf16_t>::V8 b, Acc c, int) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ Acc mma(Lanes<half_t>::V8 a, Lanes<half_t>::V8 b, Acc c) {
+__device__ __forceinline__ Acc mma(Lanes<half_t>::V8 a, Lanes<half_t>::V8 b, Acc c, int) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
-
-__device__ __forceinline__ Acc mma(Lanes<float>::V8 a, Lanes<float>::V8 b, Acc c) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[k], b[k], c, 0, 0, 0);
-  return c;
+__device__ __forceinline__ Acc mma(Lanes<float>::V8 a, Lanes<float>::V8 b, Acc c, int k) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a[k], b[k], c, 0, 0, 0);
 }
 
-// PLANES of the products: one of everything; two of dz; two of dz and of the operands
-constexpr int kOne = 1, kTwo = 2, kBoth = 3;
-constexpr int planes_of_dz(int planes) { return planes == kOne ? 1 : 2; }
+// planes of dz
+template <typename T> constexpr int kPlanes = sizeof(T) == 2 ? 2 : 1;
 
 constexpr int kFar = 0x7fffff00;       // an offset that no buffer holds: such a lane's 16 bytes read as zeros
 constexpr int64_t kReach = 0x40000000;  // what a tile's offsets stay below
@@ -273,10 +267,9 @@ __device__ __forceinline__ void wait_and_meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// O: element type of the result;  BM x BN: a block's tile of C, WM x WN waves;  STAGES: tiles in LDS, all but one of them on
-// their way (thin tiles are computed faster than one arrives)
-// PLANES: kOne, kTwo, kBoth
-template <typename T, typename O, int PLANES, int KIND, int MODE, int BM, int BN, int WM, int WN, int STAGES>
+// BM x BN: a block's tile of C, WM x WN waves;  STAGES: tiles in LDS, all but one of them on their way (thin tiles are computed
+// faster than one arrives)
+template <typename T, int KIND, int MODE, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs g) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int kWaves = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
@@ -287,8 +280,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   int tm, tn, split;
   tile_of((int)blockIdx.x, (int)gridDim.x, g.tiles_m, g.tiles_n, tm, tn, split);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-  constexpr int kPairs = PLANES == kBoth ? 3 : KIND == kLogits ? 1 : PLANES;  // products of planes
-  const int k0 = split * g.steps, ktiles = min(g.steps, g.total - k0), turns = ktiles * kPairs;
+  constexpr int kTurns = KIND == kLogits ? 1 : kPlanes<T>;  // of a tile of the summed axis: one for each plane of dz
+  const int k0 = split * g.steps, ktiles = min(g.steps, g.total - k0), turns = ktiles * kTurns;
   TA ta;
   TB tb;
   ta.init(g.a, m0, wave, lane);
@@ -299,7 +292,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   constexpr bool kTwoSums = TM * TN == 1;
   Acc total = {};
 
-  // the next fetch: tile, pair of planes, and the rows that count (read a turn ahead)
+  // the next fetch: tile, plane, and the rows that count (read a turn ahead)
   Cursor<T, KIND == kLogits> ca(g.a, m0, g.K, k0);
   Cursor<T, KIND != kWeight> cb(g.b, n0, g.K, k0);
   int lk = k0, lj = 0;
@@ -307,13 +300,12 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   const auto rows_at = [&](int k) { return rows[k * kDepth<T> / 64] >> (k * kDepth<T> % 64); };
   unsigned long long keep = KIND == kWeight ? rows_at(lk) : ~0ull;
   const auto fetch = [&](int turn) {
-    // pairs (0,0) (0,1) (1,0)
-    const int64_t pa = kPairs == 3 && lj == 2 ? ca.plane : 0, pb = kPairs > 1 && lj == 1 ? cb.plane : 0;
+    const int64_t plane = kTurns > 1 && lj == 1 ? cb.plane : 0;
     unsigned char* to = smem + turn % STAGES * kStage;
     const bool any = turn < turns;  // (behind the last tile nothing is read: zeros go where no one looks)
-    ta.fetch(ca.at + pa, any ? ca.reach() : 0, (int)g.a.ld, lk * kDepth<T>, to, wave, keep);
-    tb.fetch(cb.at + pb, any ? cb.reach() : 0, (int)g.b.ld, lk * kDepth<T>, to + TA::kBytes, wave, ~0ull);
-    if (kPairs == 1 || ++lj == kPairs) {
+    ta.fetch(ca.at, any ? ca.reach() : 0, (int)g.a.ld, lk * kDepth<T>, to, wave, keep);
+    tb.fetch(cb.at + plane, any ? cb.reach() : 0, (int)g.b.ld, lk * kDepth<T>, to + TA::kBytes, wave, ~0ull);
+    if (kTurns == 1 || ++lj == kTurns) {
       lj = 0;
       ++lk;
       ca.next();
@@ -340,10 +332,12 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
     for (int ks = 0; ks < 4; ++ks) {
       if (ks + 1 < 4) read(ks + 1);
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+      for (int k = 0; k < kMmas<T>; ++k)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mma(a[ks & 1][i], b[ks & 1][j], acc[i][j]);
-      interleave<TM * TN, TA::kReads * TM + TB::kReads * TN>();
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = mma(a[ks & 1][i], b[ks & 1][j], acc[i][j], k);
+      interleave<TM * TN * kMmas<T>, TA::kReads * TM + TB::kReads * TN>();
       if (STAGES > 1 && ks == 0) fetch(t + STAGES - 1);
     }
     if (kTwoSums && STAGES > 1 && t % 8 == 7) {
@@ -360,15 +354,6 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
   }
   wait_and_meet<0>();  // the last fetches have landed and the tiles are read: LDS is free
 
-  if constexpr (PLANES == kBoth && KIND == kLogits && MODE != kSums) {
-    const float by = g.unscale[0], by2 = g.unscale[1];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = acc[i][j][r] * by * by2;
-  }
   const int rows0 = 4 * (lane >> 5);  // accumulator r is row 8 (r / 4) + rows0 + r % 4 of its 32
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
@@ -430,7 +415,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
       using Out = Turn<T, TM>;
       unsigned char* room = smem + wave * Out::kBytes;
 #pragma unroll
-      for (int k = 0; k < planes_of_dz(PLANES); ++k) {
+      for (int k = 0; k < kPlanes<T>; ++k) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -440,7 +425,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
             for (int r = 0; r < 4; ++r) {  // (and what is left for the next plane)
               float f = acc[i][j][q * 4 + r];
               e[r] = narrow<T>(f);
-              if (PLANES != kOne) f -= widen(e[r]);
+              if (kPlanes<T> > 1) f -= widen(e[r]);
               acc[i][j][q * 4 + r] = f;
             }
             Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);
@@ -473,20 +458,20 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
             }
           }
       } else {
-        using Out = Turn<O, TM>;
+        using Out = Turn<T, TM>;
         unsigned char* room = smem + wave * Out::kBytes;
         const float scale = *g.scale;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            O e[4];
+            T e[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) e[r] = narrow<O>(acc[i][j][q * 4 + r] * scale);
+            for (int r = 0; r < 4; ++r) e[r] = narrow<T>(acc[i][j][q * 4 + r] * scale);
             Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);
           }
         const int64_t first = n0 + bn + j * 32;
-        Out::store(room, lane, static_cast<O*>(g.out) + first * g.M + m0 + am, g.M, g.N - first, g.M - m0 - am);
+        Out::store(room, lane, static_cast<T*>(g.out) + first * g.M + m0 + am, g.M, g.N - first, g.M - m0 - am);
       }
     }
   }
@@ -499,7 +484,7 @@ struct ProductPlan { int bm, bn, wm; };
 constexpr ProductPlan kPlans[] = {{256, 256, 2}, {128, 128, 2}, {128, 32, 4}, {32, 128, 1}, {64, 256, 1}, {128, 64, 4}};
 
 // g.a .. g.K, splits set; tiles, steps and total are filled in here
-template <typename T, typename O, int PLANES>
+template <typename T>
 hipError_t launch_product(int kind, int mode, int shape, ProductArgs g, hipStream_t st);
 
 }  // namespace ecc

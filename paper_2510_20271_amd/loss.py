@@ -43,7 +43,8 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
 def linear_cross_entropy(hidden, weight, labels, ignore_index: int = -100, reduction: str = "mean"):
     """hidden [..., dim] and weight [classes, dim] of one type (float32, float16 or bfloat16) on the GPU, labels [...]
     int64.  reduction "mean" (over the rows whose label is not ignore_index; 0 if there are none), "sum", or "none" (a
-    loss for each label, 0 where it is ignore_index).  The loss is float32.  Any other label outside 0 .. classes - 1
+    loss for each label, 0 where it is ignore_index).  The loss is float32, and so are sums of products, the softmax and its
+    gradient (held to twice the bits of a 16-bit type; float16: and to 2^-39 of the largest upstream gradient).  Any other label outside 0 .. classes - 1
     makes its row's loss and gradients NaN."""
     if not hidden.is_cuda or not weight.is_cuda or not labels.is_cuda:
         raise ValueError("hidden, weight and labels must be on the GPU")

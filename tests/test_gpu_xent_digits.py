@@ -7,6 +7,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
+from paper_2510_20271_amd import api
 from paper_2510_20271_amd.loss import linear_cross_entropy
 from tests.operator_bounds import E, rounding, within
 
@@ -101,9 +102,49 @@ def test_gradients_of_16_bit_heads(n, d, V, dtype, reduction):
 WIDE = [(100, 512, 2000), (128, 256, 700), (129, 512, 5000), (300, 512, 2000), (300, 511, 2000), (4097, 300, 250)]
 
 
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("n,d,V", WIDE)
+@pytest.mark.parametrize("low", [-1e6, -1e9, -1e30, -torch.finfo(torch.float32).max])
+def test_float32_with_a_masked_class(n, d, V, low):
+    """A finite weight that masks its class, at a feature that every row has."""
+    h, W, labels, up = _data(n, d, V, F32, n + V)
+    h[:, 0] = 1.0
+    W[5] = 0.0
+    W[5, 0] = low
+    labels[labels == 5] = 6
+    _check(h, W, labels, "mean", torch.tensor(0.75, device="cuda"))
+
+
+@pytest.mark.parametrize("n,d,V", WIDE)
+@pytest.mark.parametrize("power", [24, 32, 40, 60])
+def test_float32_with_one_large_row(n, d, V, power):
+    """One row of features far above the others, as a sample that diverged leaves it."""
+    h, W, labels, up = _data(n, d, V, F32, n + V)
+    h[n // 2] *= 2.0 ** power
+    _check(h, W, labels, "none", up)
+
+
+@pytest.mark.parametrize("n,d,V", WIDE)
+def test_float32_with_features_and_classes_of_many_sizes(n, d, V):
+    """Features of sizes from 1e6 to 1e-6 with weights of the inverse sizes, classes from 1 to 1e-6."""
+    h, W, labels, up = _data(n, d, V, F32, n + V)
+    by = 10.0 ** -(torch.arange(d, device="cuda") % 13 - 6).float()
+    W = W * 10.0 ** -(torch.arange(V, device="cuda") % 7).float()[:, None]
+    _check(h * by, W / by, labels, "mean", torch.tensor(0.75, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n,d,V", WIDE)
 def test_upstream_gradients_of_many_sizes(n, d, V, dtype):
     """From 1 to 1e-8 a row: each row of hidden's gradient to its own size."""
     h, W, labels, up = _data(n, d, V, dtype, n + V)
     _check(h, W, labels, "none", up * 10.0 ** -(torch.arange(n, device="cuda") % 9).float())
+
+
+def test_rows_do_not_depend_on_how_many_there_are():
+    """128 rows alone and among 300, one of them large: the same losses to a plain product's rounding."""
+    h, W, labels, up = _data(300, 512, 2000, F32, 1)
+    h[200] *= 2.0 ** 40
+    few = api.ecc_xent_fwd(h[:128].contiguous(), W, labels[:128].contiguous(), reduction="none")[0]
+    all_rows = api.ecc_xent_fwd(h, W, labels, reduction="none")[0]
+    bound = _reference(h[:128], W, labels[:128], "none", up[:128])[1]
+    assert bool(((few - all_rows[:128]).abs().double() <= 2 * bound).all())
