@@ -30,7 +30,8 @@ constexpr int kNormThreads = 512;      // of a sweep's block, at most
 constexpr int kNormFused = 1024;       // of a fused block, at most
 constexpr int kNormWide = 512;         // columns of a block, at most
 constexpr int kNormRows = 128;         // rows a thread sums, at most
-constexpr int kJoinThreads = 1024;
+constexpr int kNormJoin = 256;         // of a block that joins a group's partials
+constexpr int kJoinThreads = 1024;     // of one that joins its sums of the backward pass
 // Partials of an item that every block of the second sweep joins by itself (48 KB from the cache, 2 to 3 us) instead of a launch
 // in between (4.5 us, and as much on the host)
 constexpr int64_t kNormHere = 2048;
@@ -293,19 +294,19 @@ __device__ __forceinline__ void block_add(double& u, double& v, double (*room)[2
 }
 
 // a block for each item and group
-__global__ __launch_bounds__(256) void norm_join_kernel(const Moments* part, int nq, float eps, double* stats) {
-  __shared__ double room[4][2];
+__global__ __launch_bounds__(kNormJoin) void norm_join_kernel(const Moments* part, int nq, float eps, double* stats) {
+  __shared__ double room[kNormJoin / 64][2];
   const int64_t g = blockIdx.x;
   const Moments* m = part + g * nq;
   double n = 0.0, s = 0.0;
-  for (int i = threadIdx.x; i < nq; i += 256) {
+  for (int i = threadIdx.x; i < nq; i += kNormJoin) {
     n += m[i].n;
     s += m[i].n * m[i].mean;
   }
   block_add(n, s, room);
   const double mu = s / n;
   double q = 0.0, zero = 0.0;
-  for (int i = threadIdx.x; i < nq; i += 256) {
+  for (int i = threadIdx.x; i < nq; i += kNormJoin) {
     const double d = m[i].mean - mu;
     q += m[i].m2 + m[i].n * d * d;
   }
@@ -922,9 +923,14 @@ size_t norm_workspace_bytes(int64_t batch, int64_t points, int C, int G) {
   return norm_partials(a) + align256((size_t)batch * G * 2 * sizeof(double));
 }
 
-// items of a launch with so many blocks an item: no more threads than a grid may have
-static int64_t norm_launch(int64_t batch, int64_t blocks, unsigned threads) {
-  return std::max<int64_t>(1, std::min(batch, ((int64_t)1 << 31) / (blocks * threads)));
+// items of a launch: no more threads than a grid may have (below 2^32, the parameters' blocks with them), `item` threads an item in
+// the largest of the launches
+static int64_t norm_launch(int64_t batch, int64_t item) {
+  return std::max<int64_t>(1, std::min(batch, ((int64_t)1 << 31) / item));
+}
+// threads of an item in the sweeps, or where its groups are joined by blocks of `join` threads
+static int64_t norm_threads(const NormGeo& g, unsigned threads, int groups, int join) {
+  return std::max<int64_t>((int64_t)g.parts * g.passes * threads, (int64_t)groups * join);
 }
 
 template <typename T, int V>
@@ -935,7 +941,7 @@ static hipError_t norm_fwd_v(const NormArgs& a, hipStream_t st) {
     const unsigned threads = waves(f.wide * f.lanes);
     const size_t lds = (size_t)(f.channels / Cg) * 16 + moments_room(f.wide * f.lanes, Cg, V);
     const int slices = a.C / f.channels;
-    const int64_t each = norm_launch(a.batch, slices, threads);
+    const int64_t each = norm_launch(a.batch, (int64_t)slices * threads);
     for (int64_t n0 = 0; n0 < a.batch; n0 += each) {
       const dim3 grid((unsigned)(std::min(each, a.batch - n0) * slices));
 #define ECC_GO(KK) hipLaunchKernelGGL((norm_fused_kernel<T, V, KK>), grid, dim3(threads), lds, st, a, f, n0)
@@ -954,13 +960,14 @@ static hipError_t norm_fwd_v(const NormArgs& a, hipStream_t st) {
   Moments* part = static_cast<Moments*>(a.ws);
   double* stats = a.stats ? a.stats : reinterpret_cast<double*>(static_cast<char*>(a.ws) + norm_partials(a));
   const bool here = (int64_t)nq * a.G <= kNormHere;
-  const int64_t each = norm_launch(a.batch, (int64_t)g.parts * g.passes, threads);
+  const int64_t each = norm_launch(a.batch, norm_threads(g, threads, a.G, kNormJoin));
   for (int64_t n0 = 0; n0 < a.batch; n0 += each) {
     const int64_t items = std::min(each, a.batch - n0);
     const dim3 grid((unsigned)(items * g.parts * g.passes));
     hipLaunchKernelGGL((norm_stats_kernel<T, V>), grid, dim3(threads), moments_room(g.wide * g.lanes, Cg, V), st, a, g, n0, part);
     if (!here)
-      hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(items * a.G)), dim3(256), 0, st, part, nq, a.eps, stats + n0 * a.G * 2);
+      hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(items * a.G)), dim3(kNormJoin), 0, st, part, nq, a.eps, stats + n0 * a.G * 2);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;  // (nothing is made of statistics that are not there)
     hipLaunchKernelGGL((norm_apply_kernel<T, V>), grid, dim3(threads), here ? (size_t)a.G * 16 : 0, st, a, g, n0,
                        here ? part : nullptr, stats);
   }
@@ -977,7 +984,7 @@ static hipError_t norm_bwd_v(const NormArgs& a, hipStream_t st) {
     const unsigned threads = waves(f.wide * f.lanes);
     const size_t lds = (size_t)(f.channels / Cg) * 16 + columns_room(f, V);
     const int slices = a.C / f.channels;
-    const int64_t each = norm_launch(a.batch, slices, threads);
+    const int64_t each = norm_launch(a.batch, (int64_t)slices * threads);
     float* rows = a.batch > 1 && (a.dw || a.db) ? part : nullptr;
     NormArgs b = a;
     if (a.batch > 1) b.dw = b.db = nullptr;  // (theirs are sums over the items)
@@ -996,7 +1003,7 @@ static hipError_t norm_bwd_v(const NormArgs& a, hipStream_t st) {
   const NormGeo g = norm_geo(a, v);
   const unsigned threads = waves(g.wide * g.lanes);
   double* m12 = reinterpret_cast<double*>(static_cast<char*>(a.ws) + norm_partials(a));
-  const int64_t each = norm_launch(a.batch, (int64_t)g.parts * g.passes, threads);
+  const int64_t each = norm_launch(a.batch, norm_threads(g, threads, a.G, kJoinThreads));
   for (int64_t n0 = 0; n0 < a.batch; n0 += each) {
     const int64_t items = std::min(each, a.batch - n0);
     const dim3 grid((unsigned)(items * g.parts * g.passes));
@@ -1005,6 +1012,7 @@ static hipError_t norm_bwd_v(const NormArgs& a, hipStream_t st) {
     const bool all = items == a.batch && (a.dw || a.db);
     hipLaunchKernelGGL(norm_groups_kernel, dim3((unsigned)(items * a.G) + (all ? params : 0u)), dim3(kJoinThreads), 0, st, a, part,
                        g.parts, n0, items * a.G, m12);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL((norm_dx_kernel<T, V>), grid, dim3(threads), 0, st, a, g, n0, m12);
   }
   if ((a.dw || a.db) && (!a.dx || each < a.batch))
