@@ -397,13 +397,19 @@ int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t point
  * nothing to grad_weight.
  * Operands are multiplied as they are and summed in float32.  16-bit types hold the logits' gradient to twice their bits (float16: and
  * to 2^-39 of the largest upstream gradient).  Orders are fixed: repeated calls give the same bits.
- *   1 <= rows, classes < 2^31, 1 <= dim <= ECC_MAX_CHANNELS;  workspace: 256-byte aligned, of ecc_xent_workspace_bytes()
- *   bytes (backward: 0 or 1)
+ *   1 <= rows, classes < 2^31, 1 <= dim <= ECC_MAX_CHANNELS
+ *   workspace    256-byte aligned, of ecc_xent_workspace_bytes() bytes.  flags: ECC_XENT_BACKWARD or 0 (forward), and
+ *                ECC_XENT_ALIGNED where hidden and weight are 16-byte aligned: heads whose rows are whole 16-byte chunks then need
+ *                no copies of them (others a copy of hidden, and of up to 1 GiB of the weight, or 256 classes, at a time).  Beside copies the
+ *                backward pass takes 4 bytes for each row and up to 2^26 / rows classes (256 at the least), up to 256 MiB for
+ *                each of its split sums, and hidden's gradient in float32 where classes come in pieces
  */
 #define ECC_MEAN 0
 #define ECC_SUM 1
 #define ECC_EACH 2
-size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtype dtype, int backward);
+#define ECC_XENT_BACKWARD 1
+#define ECC_XENT_ALIGNED 2
+size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtype dtype, int flags);
 int ecc_xent_fwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,
                  ecc_dtype dtype, int64_t ignore_index, int reduction, float* loss, double* stats, int64_t* counted,
                  void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -452,8 +452,17 @@ def ecc_norm_bwd(x, grad_y, groups, stats, weight=None, bias=None, act="silu", g
     return grad_x, grad_weight, grad_bias
 
 
-def ecc_xent_workspace_bytes(rows: int, dim: int, classes: int, dtype: int, backward: bool) -> int:
-    return int(_lib.load().ecc_xent_workspace_bytes(rows, dim, classes, dtype, int(bool(backward))))
+ECC_XENT_BACKWARD, ECC_XENT_ALIGNED = 1, 2
+
+
+def ecc_xent_workspace_bytes(rows: int, dim: int, classes: int, dtype: int, backward: bool, aligned: bool = False) -> int:
+    """aligned: hidden and weight are 16-byte aligned (otherwise: enough for any alignment)."""
+    flags = ECC_XENT_BACKWARD * bool(backward) | ECC_XENT_ALIGNED * bool(aligned)
+    return int(_lib.load().ecc_xent_workspace_bytes(rows, dim, classes, dtype, flags))
+
+
+def _aligned(hidden, weight) -> bool:
+    return (hidden.data_ptr() | weight.data_ptr()) % 16 == 0
 
 
 def _xent_args(hidden, weight, labels, reduction):
@@ -486,7 +495,8 @@ def ecc_xent_fwd(hidden, weight, labels, ignore_index=-100, reduction="mean", lo
     if keep and counted is None:
         counted = torch.empty((), dtype=torch.int64, device=dev)
     if workspace is None:
-        workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, False), dev)
+        workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, False,
+                                      _aligned(hidden, weight)), dev)
     _check(_lib.load().ecc_xent_fwd(_ptr(hidden), _ptr(weight), _ptr(labels), rows, dim, classes, dtype,
                                     int(ignore_index), code, _ptr(loss), _ptr(stats), _ptr(counted), _ptr(workspace),
                                     workspace.numel(), _stream()))
@@ -511,7 +521,8 @@ def ecc_xent_bwd(hidden, weight, labels, grad_loss, stats, counted, ignore_index
     if grad_weight is None and "grad_weight" not in skip:
         grad_weight = torch.empty_like(weight)
     if workspace is None:
-        workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, True), dev)
+        workspace = _room(_kept_bytes(ecc_xent_workspace_bytes, rows, dim, classes, dtype, True,
+                                      _aligned(hidden, weight)), dev)
     _check(_lib.load().ecc_xent_bwd(_ptr(hidden), _ptr(weight), _ptr(labels), rows, dim, classes, dtype,
                                     int(ignore_index), code, _ptr(stats), _ptr(counted), _ptr(grad_loss),
                                     _ptr(grad_hidden), _ptr(grad_weight), _ptr(workspace), workspace.numel(),

@@ -594,12 +594,13 @@ static int check_xent(const ecc::XentArgs& a, int dtype, bool backward, size_t w
   if ((rc = check_array(a.stats, "stats", 16, !backward)) != ECC_OK) return rc;
   if ((rc = check_array(a.counted, "counted", 8, !backward)) != ECC_OK) return rc;
   if (!a.stats != !a.counted) return fail(ECC_ERR_INVALID_ARG, "stats and counted come together");
-  return check_workspace(a.ws, workspace_bytes, ecc::xent_workspace_bytes(a.rows, a.dim, a.classes, dtype, backward));
+  return check_workspace(a.ws, workspace_bytes, ecc::xent_workspace_bytes(a, dtype, backward));
 }
 
-size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtype dtype, int backward) {
+size_t ecc_xent_workspace_bytes(int64_t rows, int dim, int64_t classes, ecc_dtype dtype, int flags) {
   if (check_xent_sizes(rows, dim, classes, dtype) != ECC_OK) return 0;
-  return ecc::xent_workspace_bytes(rows, dim, classes, dtype, backward != 0);
+  if (flags & ~(ECC_XENT_BACKWARD | ECC_XENT_ALIGNED)) return 0;
+  return ecc::xent_workspace_bytes(rows, dim, classes, dtype, flags & ECC_XENT_BACKWARD, flags & ECC_XENT_ALIGNED);
 }
 
 int ecc_xent_fwd(const void* hidden, const void* weight, const int64_t* labels, int64_t rows, int dim, int64_t classes,

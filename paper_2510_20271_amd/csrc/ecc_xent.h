@@ -25,7 +25,9 @@ struct XentArgs {
   void* ws;
 };
 
-size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int dtype, bool backward);
+// what a call takes, and what any call of these sizes does (aligned: whose operands are 16-byte aligned)
+size_t xent_workspace_bytes(const XentArgs& a, int dtype, bool backward);
+size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int dtype, bool backward, bool aligned);
 hipError_t launch_xent_fwd(const XentArgs& a, int dtype, hipStream_t st);
 hipError_t launch_xent_bwd(const XentArgs& a, int dtype, hipStream_t st);
 

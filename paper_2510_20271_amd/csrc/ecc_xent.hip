@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int sp
 
 // ---- plans -----------------------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of two bytes of every dz (a plane of it), and of laid-out weights
-constexpr int64_t kPieceFew = (int64_t)1 << 30;      // of laid-out weights where rows are few
+constexpr int64_t kPieceFew = (int64_t)1 << 30;      // of laid-out weights where rows are few, and of any backward
 constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
 constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
 
@@ -393,7 +393,14 @@ struct XentPlan {
   size_t dz, sums_z, sums_h, sums_w, row_scale, keep, scalars;  // backward
 };
 
-static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
+// Whether the products can read the caller's own memory: rows of whole 16-byte chunks, aligned.
+static bool whole_chunks(int dim, int dtype) { return dim % (dtype == kF32 ? 4 : 8) == 0; }
+static bool as_it_is(const XentArgs& a, const void* p, int dtype) {
+  return whole_chunks(a.dim, dtype) && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
+
+// own_h, own_w: of hidden and the weight; the other needs room for a copy (the weight: of a piece)
+static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype, bool own_h, bool own_w) {
   XentPlan p{};
   const int64_t size = dtype == kF32 ? 4 : 2;
   const int planes = dtype == kF32 ? kPlanes<float> : kPlanes<half_t>, depth = 128 / (int)size;
@@ -416,7 +423,7 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   const int64_t tiles = (rows + kPlans[p.fwd_shape].bn - 1) / kPlans[p.fwd_shape].bn;
   const int64_t full = std::min((512 + tiles - 1) / tiles * kPlans[p.fwd_shape].bm, kPieceFew / (ld * size));
   p.fwd_piece = pieces(std::min(kPieceMost * 8, std::max(full, kPieceBytes / (ld * size))));
-  p.piece = pieces(std::min(kPieceMost, kPieceBytes / (rows * 2)));
+  p.piece = pieces(std::min({kPieceMost, kPieceBytes / (rows * 2), own_w ? kPieceMost : kPieceFew / (ld * size)}));
   p.ld_dz = up_to(p.piece, 8);
   p.shape = shape_of(p.piece, rows, 1, dim_turns, size == 2);
   // logits by split sums: where their tiles leave compute units idle through a long sum
@@ -433,9 +440,9 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   p.hidden_sums = p.hidden_splits > 1 || p.piece < classes;
   p.weight_shape = shape_of(dim, p.piece, long_n, rows / depth * planes, true);
   p.weight_splits = splits_of(dim, p.piece, rows, p.weight_shape, planes, depth);
-  p.lay_h = align256((size_t)rows * ld * size);
-  p.lay_w = align256((size_t)p.piece * ld * size);
-  p.lay_w_fwd = align256((size_t)p.fwd_piece * ld * size);
+  p.lay_h = own_h ? 0 : align256((size_t)rows * ld * size);
+  p.lay_w = own_w ? 0 : align256((size_t)p.piece * ld * size);
+  p.lay_w_fwd = own_w ? 0 : align256((size_t)p.fwd_piece * ld * size);
   p.part = align256((size_t)rows * p.parts * sizeof(float2));
   p.picked = p.each = align256((size_t)rows * 4);
   p.row_sums = align256(256 * sizeof(RowSum));
@@ -450,10 +457,21 @@ static XentPlan xent_plan(int64_t rows, int dim, int64_t classes, int dtype) {
   return p;
 }
 
-size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int dtype, bool backward) {
-  const XentPlan p = xent_plan(rows, dim, classes, dtype);
+static XentPlan xent_plan(const XentArgs& a, int dtype) {
+  return xent_plan(a.rows, a.dim, a.classes, dtype, as_it_is(a, a.h, dtype), as_it_is(a, a.w, dtype));
+}
+static size_t bytes_of(const XentPlan& p, bool backward) {
   if (!backward) return p.lay_h + p.lay_w_fwd + p.part + p.picked + p.each + p.row_sums + p.sums_f;
   return p.lay_h + p.lay_w + p.dz + p.sums_z + p.sums_h + p.sums_w + p.row_scale + p.keep + p.scalars;
+}
+size_t xent_workspace_bytes(const XentArgs& a, int dtype, bool backward) { return bytes_of(xent_plan(a, dtype), backward); }
+size_t xent_workspace_bytes(int64_t rows, int dim, int64_t classes, int dtype, bool backward, bool aligned) {
+  const bool whole = whole_chunks(dim, dtype);
+  if (aligned || !whole) return bytes_of(xent_plan(rows, dim, classes, dtype, whole, whole), backward);
+  size_t most = 0;  // (any alignment)
+  for (int own = 0; own < 4; ++own)
+    most = std::max(most, bytes_of(xent_plan(rows, dim, classes, dtype, own & 1, own & 2), backward));
+  return most;
 }
 
 struct Room {  // hands out a workspace
@@ -464,11 +482,6 @@ struct Room {  // hands out a workspace
     return p;
   }
 };
-
-// Whether the products can read the caller's own memory: whole elements, rows of whole 16-byte chunks.
-static bool as_it_is(const XentArgs& a, const void* p, int dtype) {
-  return a.dim % (dtype == kF32 ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
-}
 
 // An operand as the products see it, and what has to be laid out for that.
 static Matrix laid(const void* from, int64_t rows, int dim, void* room, bool own, Lay* l) {
@@ -485,7 +498,7 @@ static void prepare(const XentArgs& a, const Lay& h, const Lay& w, const Scales&
 
 template <typename T>
 static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
-  const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
+  const XentPlan p = xent_plan(a, dtype);
   Room room{static_cast<char*>(a.ws)};
   void *lay_h = room.take(p.lay_h), *lay_w = room.take(p.lay_w_fwd);
   float2* part = static_cast<float2*>(room.take(p.part));
@@ -561,7 +574,7 @@ static void xent_out(const float* sums, int splits, int64_t n, const float* scal
 
 template <typename T>
 static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
-  const XentPlan p = xent_plan(a.rows, a.dim, a.classes, dtype);
+  const XentPlan p = xent_plan(a, dtype);
   Room room{static_cast<char*>(a.ws)};
   void *lay_h = room.take(p.lay_h), *lay_w = room.take(p.lay_w), *dz = room.take(p.dz);
   float* sums_z = static_cast<float*>(room.take(p.sums_z));

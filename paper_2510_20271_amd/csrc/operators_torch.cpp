@@ -102,6 +102,11 @@ Tensor norm_act(const Tensor& x, const c10::optional<Tensor>& weight, const c10:
   return norm_forward(x, w, b, (int)groups, (float)eps, (int)act, nullptr);
 }
 
+size_t xent_room(const Tensor& h, const Tensor& w, int flags) {
+  if (((uintptr_t)h.data_ptr() | (uintptr_t)w.data_ptr()) % 16 == 0) flags |= ECC_XENT_ALIGNED;
+  return ecc_xent_workspace_bytes(h.size(0), (int)h.size(1), w.size(0), code_of(h), flags);
+}
+
 Tensor xent_forward(const Tensor& h, const Tensor& w, const Tensor& labels, int64_t ignore, int reduction, Tensor* stats,
                     Tensor* counted) {
   const int64_t rows = h.size(0), classes = w.size(0);
@@ -112,7 +117,7 @@ Tensor xent_forward(const Tensor& h, const Tensor& w, const Tensor& labels, int6
     *stats = at::empty({rows, 2}, h.options().dtype(at::kDouble));
     *counted = at::empty({}, h.options().dtype(at::kLong));
   }
-  const Tensor ws = room(ecc_xent_workspace_bytes(rows, dim, classes, code_of(h), 0), h);
+  const Tensor ws = room(xent_room(h, w, 0), h);
   check(ecc_xent_fwd(h.data_ptr(), w.data_ptr(), labels.data_ptr<int64_t>(), rows, dim, classes, code_of(h), ignore, reduction,
                      loss.data_ptr<float>(), stats ? stats->data_ptr<double>() : nullptr,
                      stats ? counted->data_ptr<int64_t>() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream()));
@@ -149,7 +154,7 @@ struct Xent : public torch::autograd::Function<Xent> {
     if (ctx->needs_input_grad(0)) dh = at::empty(h.sizes(), h.options());
     if (ctx->needs_input_grad(1)) dw = at::empty(w.sizes(), w.options());
     if (dh.defined() || dw.defined()) {
-      const Tensor ws = room(ecc_xent_workspace_bytes(rows, dim, classes, code_of(h), 1), h);
+      const Tensor ws = room(xent_room(h, w, ECC_XENT_BACKWARD), h);
       check(ecc_xent_bwd(h.data_ptr(), w.data_ptr(), labels.data_ptr<int64_t>(), rows, dim, classes, code_of(h), ignore, reduction,
                          stats.data_ptr<double>(), counted.data_ptr<int64_t>(), up.data_ptr<float>(), at_or_null(dh),
                          at_or_null(dw), ws.data_ptr(), (size_t)ws.numel(), stream()));
