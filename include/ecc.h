@@ -393,8 +393,8 @@ int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t point
  *                the label's probability
  *   counted      device int64 [1] out, the number of rows that are not left out, for ecc_xent_bwd; NULL with stats
  * ecc_xent_bwd: grad_loss (device float32, [1] or [rows] as the loss) carried on to grad_hidden and grad_weight (as hidden
- * and weight), either of which may be NULL.  Rows that are left out get zeros and, whatever their features hold, add
- * nothing to grad_weight.
+ * and weight), either of which may be NULL.  Rows that are left out get zeros, whatever weight and grad_loss
+ * hold, and add nothing to grad_weight, whatever their features hold.
  * Operands are multiplied as they are and summed in float32.  16-bit types hold the logits' gradient to twice their bits (float16: and
  * to 2^-39 of the largest upstream gradient).  Orders are fixed: repeated calls give the same bits.
  *   1 <= rows, classes < 2^31, 1 <= dim <= ECC_MAX_CHANNELS

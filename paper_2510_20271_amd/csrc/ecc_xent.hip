@@ -324,10 +324,11 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(XentArgs a, Lay h, La
   scale_rows(a, c, block - w.blocks);
 }
 
-// out = narrow(scale * sum of the splits), `team` threads to an element, added in a fixed order
+// out = narrow(scale * sum of the splits), `team` threads to an element, added in a fixed order.  labels: of out's rows of `dim`
+// elements, where those that are left out are zeros (hidden's gradient), or null
 template <typename O>
 __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int splits, int64_t n, const float* scale, int team,
-                                                       O* out) {
+                                                       const int64_t* labels, int64_t ignore, int dim, O* out) {
   __shared__ float room[256];
   const int cols = 256 / team, col = threadIdx.x % cols, lane = threadIdx.x / cols;
   const float by = *scale;
@@ -347,7 +348,10 @@ __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int sp
         __syncthreads();
       }
     }
-    if (i < n && lane == 0) out[i] = narrow<O>(s * by);
+    if (i < n && lane == 0) {
+      const int64_t row = n <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)dim) : i / dim;
+      out[i] = narrow<O>(!labels || labels[row] != ignore ? s * by : 0.0f);
+    }
   }
 }
 
@@ -566,10 +570,12 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
 }
 
 template <typename T>
-static void xent_out(const float* sums, int splits, int64_t n, const float* scale, T* out, hipStream_t st) {
+static void xent_out(const float* sums, int splits, int64_t n, const float* scale, const int64_t* labels, int64_t ignore, int dim,
+                     T* out, hipStream_t st) {
   const int team = splits >= 64 ? 16 : splits >= 16 ? 4 : 1;
   const unsigned blocks = (unsigned)std::min<int64_t>((n + 256 / team - 1) / (256 / team), 4096);
-  hipLaunchKernelGGL(xent_out_kernel<T>, dim3(blocks), dim3(256), 0, st, sums, splits, n, scale, team, out);
+  hipLaunchKernelGGL(xent_out_kernel<T>, dim3(blocks), dim3(256), 0, st, sums, splits, n, scale, team, labels,
+                     ignore, dim, out);
 }
 
 template <typename T>
@@ -628,10 +634,11 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
       g.out = out;
       g.scale = scale;
       if ((e = launch_product<T>(kWeight, 0, p.weight_shape, g, st)) != hipSuccess) return e;
-      if (g.sums) xent_out(sums_w, p.weight_splits, count * a.dim, scale, out, st);
+      if (g.sums) xent_out(sums_w, p.weight_splits, count * a.dim, scale, nullptr, 0, a.dim, out, st);
     }
   }
-  if (a.dh && p.hidden_sums) xent_out(sums_h, p.hidden_splits, a.rows * a.dim, scale, static_cast<T*>(a.dh), st);
+  if (a.dh && p.hidden_sums)
+    xent_out(sums_h, p.hidden_splits, a.rows * a.dim, scale, a.labels, a.ignore, a.dim, static_cast<T*>(a.dh), st);
   return hipGetLastError();
 }
 

@@ -46,7 +46,7 @@ struct ProductArgs {
   int add;             //   added to what is there
   void* out;           // [N][M], scaled by *scale
   const float* scale;  // [1]
-  // kLogits
+  // kLogits; kHidden: rows that are left out are zeros, whatever weights and scale hold
   const int64_t* labels;
   int64_t v0;          // the first class of this piece (M: its classes)
   float2* part;        // forward: [N][parts], parts part0 ..: the maximum, and the sum of exponentials but the label's
@@ -461,13 +461,14 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
         using Out = Turn<T, TM>;
         unsigned char* room = smem + wave * Out::kBytes;
         const float scale = *g.scale;
+        const bool counts = KIND != kHidden || (in && g.labels[n] != g.ignore);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             T e[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) e[r] = narrow<T>(acc[i][j][q * 4 + r] * scale);
+            for (int r = 0; r < 4; ++r) e[r] = narrow<T>(counts ? acc[i][j][q * 4 + r] * scale : 0.0f);
             Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);
           }
         const int64_t first = n0 + bn + j * 32;
