@@ -284,22 +284,23 @@ struct Scales {
   const float* top;  // float16 with a gradient for each row: the largest of them
   float* row_scale;
   unsigned long long* keep;
-  float* scale;      // [1]: of both gradients
+  float* scale;      // [2]: of both gradients: a factor and an exponent, which would be subnormal as one number where they are not
   bool half;         // dz is held in float16
   int64_t blocks;    // 0: none wanted
 };
 __device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, int64_t block) {
   const int64_t i = block * 256 + threadIdx.x;
-  float by = c.half ? kHalfScale : 1.0f, back = 1.0f / by;
+  float by = c.half ? kHalfScale : 1.0f;
+  double back = 1.0 / (double)by;
   if (a.reduction == kEach) {
     if (c.half) {
       const float t = c.top[0] > 0.0f ? fmaxf(c.top[0], 0x1p-100f) : 1.0f;  // (kHalfScale / t stays finite)
       by /= t;
-      back *= t;
+      back *= (double)t;
     }
   } else {
-    back *= a.up[0];
-    if (a.reduction == kMean) back /= (float)(a.counted[0] > 0 ? a.counted[0] : 1);
+    back *= (double)a.up[0];
+    if (a.reduction == kMean) back /= (double)(a.counted[0] > 0 ? a.counted[0] : 1);
   }
   bool counts = false;
   if (i < a.rows) {
@@ -311,7 +312,12 @@ __device__ __forceinline__ void scale_rows(const XentArgs& a, const Scales& c, i
   }
   const unsigned long long bits = __ballot(counts);
   if ((threadIdx.x & 63) == 0 && i < a.rows) c.keep[i / 64] = bits;
-  if (i == 0) c.scale[0] = back;
+  if (i == 0) {
+    int e = 0;
+    const bool finite = fabs(back) < (double)INFINITY;
+    c.scale[0] = finite ? (float)frexp(back, &e) : (float)back;
+    c.scale[1] = (float)e;
+  }
 }
 
 // What comes before the products, in one launch: both operands laid out and the rows' scales, a run of blocks each.
@@ -324,14 +330,15 @@ __global__ __launch_bounds__(256) void xent_prepare_kernel(XentArgs a, Lay h, La
   scale_rows(a, c, block - w.blocks);
 }
 
-// out = narrow(scale * sum of the splits), `team` threads to an element, added in a fixed order.  labels: of out's rows of `dim`
+// out = narrow(scale[0] 2^scale[1] * sum of the splits), `team` threads to an element, added in a fixed order.  labels: of out's rows of `dim`
 // elements, where those that are left out are zeros (hidden's gradient), or null
 template <typename O>
 __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int splits, int64_t n, const float* scale, int team,
                                                        const int64_t* labels, int64_t ignore, int dim, O* out) {
   __shared__ float room[256];
   const int cols = 256 / team, col = threadIdx.x % cols, lane = threadIdx.x / cols;
-  const float by = *scale;
+  const float by = scale[0];
+  const int exponent = (int)scale[1];
   for (int64_t i0 = (int64_t)blockIdx.x * cols; i0 < n; i0 += (int64_t)gridDim.x * cols) {  // (block-uniform)
     const int64_t i = i0 + col;
     float s = 0.0f;
@@ -350,7 +357,7 @@ __global__ __launch_bounds__(256) void xent_out_kernel(const float* sums, int sp
     }
     if (i < n && lane == 0) {
       const int64_t row = n <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)dim) : i / dim;
-      out[i] = narrow<O>(!labels || labels[row] != ignore ? s * by : 0.0f);
+      out[i] = narrow<O>(!labels || labels[row] != ignore ? ldexpf(s * by, exponent) : 0.0f);
     }
   }
 }
@@ -592,8 +599,8 @@ static hipError_t xent_bwd(const XentArgs& a, int dtype, hipStream_t st) {
   const T *h = static_cast<const T*>(a.h), *w = static_cast<const T*>(a.w);
   const bool half = dtype == kF16;
   if (half && a.reduction == kEach)
-    hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a, scale + 1);
-  Scales scales{scale + 1, row_scale, keep, scale, half, (a.rows + 255) / 256};
+    hipLaunchKernelGGL(xent_top_kernel, dim3(1), dim3(kSumThreads), 0, st, a, scale + 2);
+  Scales scales{scale + 2, row_scale, keep, scale, half, (a.rows + 255) / 256};
   Lay lh, lw;
   const Matrix hm = laid(h, a.rows, a.dim, lay_h, as_it_is(a, h, dtype), &lh);
   const bool own = as_it_is(a, w, dtype);

@@ -44,8 +44,8 @@ struct ProductArgs {
   // results
   float* sums;         // kHidden, kWeight, kSums: [splits][N][M], or null: straight to out
   int add;             //   added to what is there
-  void* out;           // [N][M], scaled by *scale
-  const float* scale;  // [1]
+  void* out;           // [N][M], times scale[0] 2^scale[1]
+  const float* scale;
   // kLogits; kHidden: rows that are left out are zeros, whatever weights and scale hold
   const int64_t* labels;
   int64_t v0;          // the first class of this piece (M: its classes)
@@ -460,7 +460,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
       } else {
         using Out = Turn<T, TM>;
         unsigned char* room = smem + wave * Out::kBytes;
-        const float scale = *g.scale;
+        const float scale = g.scale[0];
+        const int exponent = (int)g.scale[1];
         const bool counts = KIND != kHidden || (in && g.labels[n] != g.ignore);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(const ProductArgs
           for (int q = 0; q < 4; ++q) {
             T e[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) e[r] = narrow<T>(counts ? acc[i][j][q * 4 + r] * scale : 0.0f);
+            for (int r = 0; r < 4; ++r) e[r] = narrow<T>(counts ? ldexpf(acc[i][j][q * 4 + r] * scale, exponent) : 0.0f);
             Out::put(room, lane & 31, i * 32 + 8 * q + rows0, e);
           }
         const int64_t first = n0 + bn + j * 32;

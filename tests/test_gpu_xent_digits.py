@@ -148,3 +148,25 @@ def test_rows_do_not_depend_on_how_many_there_are():
     all_rows = api.ecc_xent_fwd(h, W, labels, reduction="none")[0]
     bound = _reference(h[:128], W, labels[:128], "none", up[:128])[1]
     assert bool(((few - all_rows[:128]).abs().double() <= 2 * bound).all())
+
+
+# hidden's gradient and the weight's straight from their products, from split sums, and from several pieces of the classes
+@pytest.mark.parametrize("n,d,V", [(41, 20, 30), (9, 64, 5000), (300, 512, 2000), (4100, 16, 33000), (5000, 64, 21)])
+@pytest.mark.parametrize("up", [1.3 * 2.0 ** -126, 1.7 * 2.0 ** -120, 0.75, 1.3 * 2.0 ** 100])
+def test_float32_upstream_gradients_of_any_size(n, d, V, up):
+    """A mean's upstream gradient over a count that is no power of two: their quotient may have no digits of its own where the gradients
+    have all of theirs."""
+    h, W, labels, _ = _data(n, d, V, F32, n + V)
+    labels[0] = 1
+    far = 2.0 ** 40 if up < 1e-30 else 2.0 ** -40  # (logits are the same)
+    up = torch.tensor(up, device="cuda")
+    for by in (1.0, far, 1.0 / far):
+        hr, Wr = (h * by).requires_grad_(True), (W / by).requires_grad_(True)
+        loss = linear_cross_entropy(hr, Wr, labels)
+        grads = torch.autograd.grad(loss, (hr, Wr), up)
+        ref = _reference(hr.detach(), Wr.detach(), labels, "mean", up)
+        within(loss.detach(), ref[0], ref[1], "loss")
+        for got, want, bound, name in zip(grads, ref[2::2], ref[3::2], ("dhidden", "dweight")):
+            beyond = want.abs() + bound > torch.finfo(F32).max  # (features of 1e12 and an upstream gradient of 1e30)
+            assert bool((got[want.abs() - bound > torch.finfo(F32).max].abs() == math.inf).all())
+            within(torch.where(beyond, 0.0, got), torch.where(beyond, 0.0, want), bound, name)
