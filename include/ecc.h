@@ -397,7 +397,7 @@ int ecc_norm_bwd(const void* x, const void* grad_y, int64_t batch, int64_t point
  * hold, and add nothing to grad_weight, whatever their features hold.
  * Operands are multiplied as they are and summed in float32.  16-bit types hold the logits' gradient to twice their bits (float16: and
  * to 2^-39 of the largest upstream gradient).  Orders are fixed: repeated calls give the same bits.
- *   1 <= rows, classes < 2^31, 1 <= dim <= ECC_MAX_CHANNELS
+ *   1 <= rows, classes <= 2^31 - 256, 1 <= dim <= ECC_MAX_CHANNELS
  *   workspace    256-byte aligned, of ecc_xent_workspace_bytes() bytes.  flags: ECC_XENT_BACKWARD or 0 (forward), and
  *                ECC_XENT_ALIGNED where hidden and weight are 16-byte aligned: heads whose rows are whole 16-byte chunks then need
  *                no copies of them (others a copy of hidden, and of up to 1 GiB of the weight, or 256 classes, at a time).  Beside copies the

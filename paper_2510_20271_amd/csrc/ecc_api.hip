@@ -578,8 +578,8 @@ static int check_xent_sizes(int64_t rows, int dim, int64_t classes, int dtype) {
   if (rows < 1 || classes < 1 || dim < 1)
     return fail(ECC_ERR_INVALID_ARG, "rows, dim and classes must be >= 1, got %lld, %d, %lld", (long long)rows, dim,
                 (long long)classes);
-  if (rows > INT32_MAX || classes > INT32_MAX || dim > ECC_MAX_CHANNELS)
-    return fail(ECC_ERR_UNSUPPORTED, "rows and classes must be below 2^31 and dim at most %d", ECC_MAX_CHANNELS);
+  if (rows > INT32_MAX - 255 || classes > INT32_MAX - 255 || dim > ECC_MAX_CHANNELS)
+    return fail(ECC_ERR_UNSUPPORTED, "rows and classes must be at most 2^31 - 256 and dim at most %d", ECC_MAX_CHANNELS);
   return check_operator_dtype(dtype);
 }
 static int check_xent(const ecc::XentArgs& a, int dtype, bool backward, size_t workspace_bytes) {

@@ -87,8 +87,8 @@ __device__ __forceinline__ float xent_row(const XentArgs& a, int64_t row, float 
 }
 // A row's tiles joined by `team` lanes (a power of two).
 __global__ __launch_bounds__(256) void xent_rows_kernel(XentArgs a, const float2* part, const float* picked, float* each,
-                                                        int64_t parts, int team) {
-  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / team;
+                                                        int64_t parts, int team, int64_t row0) {
+  const int64_t row = row0 + ((int64_t)blockIdx.x * 256 + threadIdx.x) / team;
   const int lane = threadIdx.x & (team - 1);
   const bool in = row < a.rows;  // (whole waves take part in the exchanges)
   const float2* p = part + (in ? row : 0) * parts;
@@ -367,6 +367,7 @@ constexpr int64_t kPieceBytes = (int64_t)128 << 20;  // of two bytes of every dz
 constexpr int64_t kPieceFew = (int64_t)1 << 30;      // of laid-out weights where rows are few, and of any backward
 constexpr int64_t kPieceMost = (int64_t)1 << 17;     // classes of a piece (offsets within a tile are 32 bits)
 constexpr int64_t kSumsBytes = (int64_t)256 << 20;   // of the splits' results
+constexpr int64_t kLaunchThreads = (int64_t)1 << 31; // of a launch (a grid may have less than 2^32)
 
 static int ld_of(int dim) { return (int)up_to(dim, 8); }
 
@@ -532,9 +533,9 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   g.picked = picked;
   const bool own = as_it_is(a, w, dtype);
   const ProductPlan& plan = kPlans[p.fwd_shape];
-  // (all classes at once where nothing is laid out, but no more blocks than a grid may have)
-  const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 22) / ((a.rows + plan.bn - 1) / plan.bn)) * plan.bm;
-  const int64_t piece = p.fwd_splits > 1 ? a.classes : std::min(own ? a.classes : p.fwd_piece, std::max<int64_t>(256, most / 256 * 256));
+  // (all classes at once where nothing is laid out, but no more threads than a grid may have: whole tiles, of up to 512 each)
+  const int64_t most = std::max<int64_t>(1, kLaunchThreads / 512 / ((a.rows + plan.bn - 1) / plan.bn)) * plan.bm;
+  const int64_t piece = p.fwd_splits > 1 ? a.classes : std::min(own ? a.classes : p.fwd_piece, most);
   hipError_t e = hipSuccess;
   for (int64_t v0 = 0; v0 < a.classes && e == hipSuccess; v0 += piece) {
     const int64_t count = std::min(piece, a.classes - v0);
@@ -564,8 +565,11 @@ static hipError_t xent_fwd(const XentArgs& a, int dtype, hipStream_t st) {
   } else {
     // (one lane of a team ends its row, in float64: no larger teams than fill the card)
     while (team > 1 && a.rows * (team / 2) >= 131072 && p.parts <= 4 * team) team /= 2;
-    hipLaunchKernelGGL(xent_rows_kernel, dim3((unsigned)((a.rows * team + 255) / 256)), dim3(256), 0, st, a, part, picked, each,
-                       p.parts, team);
+    const int64_t step = kLaunchThreads / team;
+    for (int64_t r0 = 0; r0 < a.rows; r0 += step) {
+      const unsigned blocks = (unsigned)((std::min(step, a.rows - r0) * team + 255) / 256);
+      hipLaunchKernelGGL(xent_rows_kernel, dim3(blocks), dim3(256), 0, st, a, part, picked, each, p.parts, team, r0);
+    }
   }
   if (a.reduction != kEach || a.counted) {
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(256, a.rows / 8192));

@@ -51,3 +51,18 @@ def test_exact_workspaces(n, d, V, dtype, code, shift_h, shift_w):
             with pytest.raises(api.EccError) as e:
                 call(_workspace(size, 0)[1][:size - 1])
             assert e.value.status == -3
+
+
+def test_more_tiles_than_one_launch_takes():
+    """2^30 rows: two tiles of classes for each tile of rows would be a grid of 2^32 threads."""
+    n, d, V = (1 << 30) + 300, 8, 200
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    W = torch.randn(V, d, generator=gen, device="cuda").to(torch.bfloat16)
+    h = torch.empty(n, d, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    labels = torch.randint(0, V, (n,), generator=gen, device="cuda")
+    loss = api.ecc_xent_fwd(h, W, labels, reduction="none", keep=False)[0]
+    for part in (slice(0, 300), slice((1 << 29) - 150, (1 << 29) + 150), slice(n - 600, n)):
+        ref = _reference(h[part], W, labels[part], "none", torch.ones(len(loss[part]), device="cuda"))
+        within(loss[part], ref[0], ref[1], "loss")
+    del h, labels, loss
+    torch.cuda.empty_cache()

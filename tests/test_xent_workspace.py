@@ -50,3 +50,12 @@ def test_flags():
                 assert 0 < aligned <= any_alignment
                 assert (aligned == any_alignment) == (dim % (4 if dtype == F32 else 8) != 0)
     assert query(4, 8, 16, F32, 4) == 0 and query(4, 8, 16, F32, -1) == 0
+
+
+def test_largest_sizes():
+    """Rows and classes up to 2^31 - 256: one tile of the smallest kind more would be a grid of 2^32 threads."""
+    for back in (0, 1):
+        assert _lib.load().ecc_xent_workspace_bytes(2 ** 31 - 256, 1, 2, F32, back) > 0
+        for rows, classes in ((2 ** 31 - 255, 2), (2, 2 ** 31 - 255)):
+            assert _lib.load().ecc_xent_workspace_bytes(rows, 1, classes, F32, back) == 0
+            assert "2^31 - 256" in _lib.load().ecc_last_error().decode()
