@@ -361,7 +361,8 @@ int ecc_count_nonfinite(const void* grid, int64_t n, ecc_dtype dtype, unsigned l
  * ecc_norm_bwd: from x, stats and the upstream gradient grad_y (as y) the gradients grad_x (as x), grad_weight and
  * grad_bias (device float32 [channels]); any of the three may be NULL, not all.  The derivative of relu at 0 is 0.
  * Sums are float32 within a block's share and float64 beyond, in a fixed order: repeated calls give the same bits.  Outputs
- * must not overlap inputs.  A NaN or Inf spoils its own group of its own item, and the gradients of its channels.
+ * must not overlap inputs.  A NaN or Inf spoils its own group of its own item, and grad_weight of its channels (with
+ * ECC_ACT_SILU grad_bias too).
  *   1 <= channels <= ECC_MAX_CHANNELS, groups a divisor of channels, eps finite and >= 0
  *   workspace    ecc_norm_workspace_bytes() bytes, 256-byte aligned, enough for either call
  */

@@ -2,9 +2,10 @@
 //   z_iv = <h_i, W_v>,   lse_i = log sum_v exp z_iv,   loss_i = lse_i - z_{i,label},
 //   dz_iv = (exp(z_iv - lse_i) - [v = label_i]) g_i,   dh = dz W,   dW = dz^T h.
 // The logits are never kept: the forward pass leaves a maximum and a sum for each row and tile of classes, the backward pass
-// forms dz of one piece of the classes at a time, in the operands' type, for the two products that read it.
+// forms dz of one piece of the classes at a time, in planes of the operands' type, for the two products that read it.
 //
-// Matrix products bound it (ecc_xent_product.h): rows x dim x classes multiply-adds forward, three times that backward.
+// Matrix products bound it (ecc_xent_product.h): rows x dim x classes multiply-adds forward; backward three times that in float32, five
+// times in 16-bit types, whose dz has two planes.
 #include "ecc_xent.h"
 
 #include <algorithm>
@@ -16,16 +17,16 @@
 namespace ecc {
 
 // float16 holds dz as a multiple of 2^-14 of the largest upstream gradient: the probabilities of a large vocabulary are far below its
-// least number otherwise.  (They are at most 1: 2^14 is in range.  Values are good to 2^-39 of
-// the largest.)
+// least number otherwise.  (They are at most 1: 2^14 is in range.  Two planes are good to 2^-39 of the largest, half a step of
+// float16's least numbers wherever that gradient times a column's sum of weights is below 2^14.)
 constexpr float kHalfScale = 16384.0f;
 
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 static int64_t up_to(int64_t n, int64_t k) { return (n + k - 1) / k * k; }
 
 // ---- operands --------------------------------------------------------------------------------------------------------------
-// One operand to be laid out as the products take them: [rows][ld], zeros behind a row's end.  blocks: 0 where the
-// caller's own memory will do.
+// One operand to be laid out as the products take them: [rows][ld], zeros behind a row's end.  blocks: 0 where the caller's own
+// memory will do.
 struct Lay {
   const void* from;
   void* to;

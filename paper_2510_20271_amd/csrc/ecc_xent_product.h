@@ -236,7 +236,7 @@ struct Turn {
     }
   }
   // rows and columns that are there; out: element (0, 0), rows `ld` apart, of any alignment (142 x 1863 x 56007 in float16, gradient
-  // of the weight: 243 us with stores of an element each for such rows, 113 so)
+  // of the weight: 290 us with stores of an element each for such rows, 167 so)
   __device__ __forceinline__ static void store(unsigned char* room, int lane, E* out, int64_t ld, int64_t rows, int64_t columns) {
 #pragma unroll
     for (int k = 0; k < kChunks / 2; ++k) {
